@@ -650,7 +650,7 @@ hipError_t launch_reduce_t(const DecodeArgs &a, hipStream_t stream, const Kernel
 
 bool decode_args_ok(const DecodeArgs &a, int tblk) {
     if (!(a.T > (tblk - 1) * 16 && a.T <= tblk * 16 && a.K > 0 && (a.K & 7) == 0 && a.nbe >= 0 && a.nbe <= a.nbe_cap && a.X != nullptr &&
-          a.ks == (a.K / 8 + kDsSliceChunks - 1) / kDsSliceChunks && a.n_sets >= 0 && a.n_sets <= kMaxGemmSets))
+          a.slice_chunks > 0 && a.ks == (a.K / 8 + a.slice_chunks - 1) / a.slice_chunks && a.n_sets >= 0 && a.n_sets <= kMaxGemmSets))
         return false;
     if (a.n_sets == 0) return a.N > 0 && a.nbw == (a.N + 15) / 16 && a.P != nullptr && a.W != nullptr && a.Y != nullptr;
     for (int i = 0; i < a.n_sets; ++i) {
@@ -676,7 +676,7 @@ hipError_t init_decode_kernels() {
 
 // tblk: 16-row blocks of the batch (1 .. 8).
 hipError_t launch_decode_stream(const DecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer) {
-    if (!decode_args_ok(a, tblk)) return hipErrorInvalidValue;
+    if (!decode_args_ok(a, tblk) || a.slice_chunks != kDsSliceChunks) return hipErrorInvalidValue;
     switch (tblk) {
         case 1:
             return launch_stream_t<1, kDecodeMaxWaves>(a, stream, timer);

@@ -12,6 +12,7 @@
 
 #include "../../include/lora_mi355x.h"
 #include "kernels.h"
+#include "mx_kernels.h"
 
 using namespace lora;
 
@@ -1141,6 +1142,8 @@ int lora_ctx_create(lora_ctx **out, int device_ordinal) {
     if (e == hipSuccess) e = init_decode_kernels();
     if (e == hipSuccess) e = init_shrink_kernels();
     if (e == hipSuccess) e = init_expand_kernels();
+    if (e == hipSuccess) e = init_mx_decode_kernels();
+    if (e == hipSuccess) e = init_mx_gemm_kernels();
     if (e == hipSuccess) e = hipGetSymbolAddress(reinterpret_cast<void **>(&ctx->static_scratch), HIP_SYMBOL(scratch));
     if (e != hipSuccess) {
         for (int i = 0; i < kRingSlots; ++i)
@@ -1583,3 +1586,5 @@ const char *lora_strerror(int status) {
 int lora_last_hip_error(void) { return g_last_hip_error; }
 
 }  // extern "C"
+
+#include "mx_api.hiph"

@@ -1,0 +1,96 @@
+// Host-side launch interface between mx_api.hiph and the kernels on block-scaled formats.
+#pragma once
+#include "kernels.h"
+
+namespace lora {
+
+constexpr int kMxBlock = 32;
+constexpr int kMxPieces = 4;               // of 64 x 8 values that a wave of the conversions takes: that many loads in flight
+constexpr int kMxStrip = kMxPieces * 512;  // (rows x strips of a conversion stay below 2^31)
+enum MxFormat { kMxE2M1 = 0, kMxE4M3 = 1 };
+
+struct MxConvertArgs {
+    const void *src;  // quantize: values; dequantize: codes
+    int64_t lds;      // elements (values) or bytes (codes) from row to row
+    void *dst;        // the other of the two
+    int64_t ldd;
+    unsigned char *scales;  // written by quantize, read by dequantize
+    int64_t ldsc;
+    int64_t rows;
+    int32_t K;
+    int32_t strips;   // pieces of a row that a wave takes (set by the launcher)
+};
+hipError_t launch_mx_quantize(const MxConvertArgs &a, int dtype, int format, hipStream_t stream, const KernelTimer *timer);
+hipError_t launch_mx_dequantize(const MxConvertArgs &a, int dtype, int format, hipStream_t stream, const KernelTimer *timer);
+
+struct RmsNormArgs {
+    const void *X;
+    int64_t ldx;
+    const void *R;  // null: none
+    int64_t ldr;
+    const void *gamma;
+    void *H;        // null: none
+    int64_t ldh;
+    void *Y;        // null: none
+    int64_t ldy;
+    unsigned char *codes;  // null: none
+    int64_t ldc;
+    unsigned char *scales;
+    int64_t ldsc;
+    int64_t rows;
+    int32_t K;
+    float eps;
+};
+hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, int num_cu, hipStream_t stream, const KernelTimer *timer);
+
+// Decode-sized batches: the streaming launch of the decode path on 4-bit weights; the second launch is the decode path's own.
+struct MxDecodeSet {
+    const unsigned char *Wq;
+    int64_t ldwq;
+    const unsigned char *Ws;
+    int64_t ldws;
+    int32_t group0;  // first group of workgroups of this projection (set by the launcher)
+    int32_t pad_;
+};
+struct MxDecodeArgs {
+    DecodeArgs d;                // set[0 .. n) in use whatever n_sets says; ks counts slices of slice_chunks
+    const unsigned char *Xq;     // null: d.X
+    int64_t ldxq;
+    const unsigned char *Xs;
+    int64_t ldxs;
+    int32_t n;                   // projections
+    int32_t ext_groups;          // per projection (set by the launcher)
+    MxDecodeSet w[kMaxGemmSets];
+};
+constexpr int kMxWideBlocks = 4;  // most 16-row blocks of a batch whose X slices of 1024 values fit into LDS
+hipError_t init_mx_decode_kernels();
+hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
+
+// More rows: tiles on 4-bit weights and 8-bit activations.
+struct MxGemmSet {
+    const unsigned char *Wq;
+    int64_t ldwq;
+    const unsigned char *Ws;
+    int64_t ldws;
+    void *Y;
+    int64_t ldy;
+    const float *D;  // adapter term in fp32, [T, ldd], rows with an adapter only (null: none)
+    int64_t ldd;
+    int32_t N;
+    int32_t tile0;   // first column tile (set by the launcher)
+};
+struct MxGemmArgs {
+    PlanView plan;
+    const unsigned char *Xq;
+    int64_t ldxq;
+    const unsigned char *Xs;
+    int64_t ldxs;
+    int32_t T, K;
+    int32_t n_sets;
+    int32_t pad_;
+    MxGemmSet set[kMaxGemmSets];
+};
+hipError_t init_mx_gemm_kernels();
+hipError_t launch_mx_gemm(const MxGemmArgs &a, int variant, hipStream_t stream, const KernelTimer *timer);
+
+}  // namespace lora

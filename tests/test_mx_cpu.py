@@ -1,0 +1,200 @@
+"""include/lora_mx.h without a GPU: the library exports what the header declares, descriptors have the C compiler's layout, and every
+refusal comes before the first HIP call.  Pins of the oracle of the block-scaled formats."""
+import ctypes as C
+import os
+import re
+
+import numpy as np
+import pytest
+
+from oracle import mx_reference as ref
+from paper_2505_14468_amd import binding as B
+from paper_2505_14468_amd import mx
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_exports_match_the_header():
+    text = open(os.path.join(ROOT, "include", "lora_mx.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = sorted(set(re.findall(r"\b(lora_[a-z_]+)\s*\(", text)))
+    assert names == sorted(mx.EXPORTS)
+    for n in names:
+        assert hasattr(mx.lib(), n), n
+    for name in ("LORA_MX_E2M1", "LORA_MX_E4M3"):
+        assert getattr(mx, name) == int(re.search(name + r" = (\d+)", text)[1])
+    for name in ("LORA_MX_BLOCK", "LORA_RMS_NORM_MAX_K"):
+        assert getattr(mx, name) == int(re.search(name + r" (\d+)", text)[1])
+
+
+def test_struct_layouts_match_c():
+    assert C.sizeof(mx.lora_mx_rows_t) == 40
+    assert C.sizeof(mx.lora_mx_convert_desc) == 72
+    assert C.sizeof(mx.lora_rms_norm_desc) == 136
+    assert C.sizeof(mx.lora_mx_linear_desc) == 152
+
+
+# Addresses far apart: nothing is dereferenced, every call is refused (or a no-op) before the GPU is touched.
+AT = [(i + 1) << 44 for i in range(10)]
+
+
+def _rows(at, ld, scales, lds, fmt=mx.LORA_MX_E4M3):
+    return mx.lora_mx_rows_t(at, ld, scales, lds, fmt, 0)
+
+
+def _convert(**kw):
+    f = dict(dtype=1, K=64, rows=5, X=AT[0], ldx=64, q=_rows(AT[1], 64, AT[2], 4))
+    f.update(kw)
+    return mx.lora_mx_convert_desc(*f.values())
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(), B.LORA_ERR_INVALID_ARG),  # (all is well but the context)
+    (dict(dtype=2), B.LORA_ERR_INVALID_ARG), (dict(rows=-1), B.LORA_ERR_INVALID_ARG), (dict(X=0), B.LORA_ERR_INVALID_ARG),
+    (dict(K=0), B.LORA_ERR_SHAPE), (dict(K=40, ldx=40), B.LORA_ERR_SHAPE), (dict(ldx=56), B.LORA_ERR_SHAPE), (dict(ldx=68), B.LORA_ERR_ALIGNMENT),
+    (dict(X=AT[0] + 8), B.LORA_ERR_ALIGNMENT), (dict(rows=2 ** 31), B.LORA_ERR_SHAPE), (dict(ldx=2 ** 60), B.LORA_ERR_SHAPE),
+    (dict(q=_rows(AT[1], 48, AT[2], 4)), B.LORA_ERR_SHAPE), (dict(q=_rows(AT[1], 72, AT[2], 4)), B.LORA_ERR_ALIGNMENT),
+    (dict(q=_rows(AT[1], 64, AT[2], 2)), B.LORA_ERR_ALIGNMENT), (dict(q=_rows(AT[1], 64, AT[2], 0)), B.LORA_ERR_SHAPE),
+    (dict(q=_rows(AT[1], 64, AT[2] + 2, 4)), B.LORA_ERR_ALIGNMENT), (dict(q=_rows(AT[1] + 8, 64, AT[2], 4)), B.LORA_ERR_ALIGNMENT),
+    (dict(q=_rows(0, 64, AT[2], 4)), B.LORA_ERR_INVALID_ARG), (dict(q=_rows(AT[1], 64, 0, 4)), B.LORA_ERR_INVALID_ARG),
+    (dict(q=_rows(AT[1], 64, AT[2], 4, 2)), B.LORA_ERR_INVALID_ARG), (dict(q=mx.lora_mx_rows_t(AT[1], 64, AT[2], 4, 1, 1)), B.LORA_ERR_INVALID_ARG),
+    (dict(q=_rows(AT[0] + 64 * 9, 64, AT[2], 4)), B.LORA_ERR_INVALID_ARG), (dict(q=_rows(AT[1], 64, AT[0] + 16, 4)), B.LORA_ERR_INVALID_ARG),
+    (dict(q=_rows(AT[1], 64, AT[1] + 64, 4)), B.LORA_ERR_INVALID_ARG),
+])
+def test_conversion_refusals(kw, status):
+    for call in (mx.lora_mx_quantize, mx.lora_mx_dequantize):
+        assert call(None, _convert(**kw), None, raw=True) == status
+    assert mx.lib().lora_mx_quantize(None, None, None) == B.LORA_ERR_INVALID_ARG
+
+
+def _norm(**kw):
+    f = dict(dtype=1, K=64, rows=5, eps=1e-5, flags=0, X=AT[0], ldx=64, R=AT[1], ldr=64, gamma=AT[2], H=AT[3], ldh=64, Y=AT[4], ldy=64,
+             q=_rows(AT[5], 64, AT[6], 4))
+    f.update(kw)
+    return mx.lora_rms_norm_desc(*f.values())
+
+
+NOQ = _rows(None, 0, None, 0)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=7), B.LORA_ERR_INVALID_ARG), (dict(rows=-1), B.LORA_ERR_INVALID_ARG), (dict(rows=2 ** 31), B.LORA_ERR_INVALID_ARG),
+    (dict(flags=1), B.LORA_ERR_INVALID_ARG), (dict(eps=-1.0), B.LORA_ERR_INVALID_ARG), (dict(eps=float("nan")), B.LORA_ERR_INVALID_ARG),
+    (dict(eps=float("inf")), B.LORA_ERR_INVALID_ARG), (dict(X=0), B.LORA_ERR_INVALID_ARG), (dict(gamma=0), B.LORA_ERR_INVALID_ARG),
+    (dict(K=0), B.LORA_ERR_SHAPE), (dict(K=60), B.LORA_ERR_SHAPE), (dict(K=40), B.LORA_ERR_SHAPE), (dict(K=65568), B.LORA_ERR_SHAPE),
+    (dict(H=0, Y=0, q=NOQ), B.LORA_ERR_INVALID_ARG), (dict(ldx=56), B.LORA_ERR_SHAPE), (dict(ldr=56), B.LORA_ERR_SHAPE),
+    (dict(ldh=56), B.LORA_ERR_SHAPE), (dict(ldy=56), B.LORA_ERR_SHAPE), (dict(ldr=68), B.LORA_ERR_ALIGNMENT), (dict(Y=AT[4] + 4), B.LORA_ERR_ALIGNMENT),
+    (dict(gamma=AT[2] + 2), B.LORA_ERR_ALIGNMENT), (dict(q=_rows(AT[5], 64, AT[6], 4, mx.LORA_MX_E2M1)), B.LORA_ERR_INVALID_ARG),
+    (dict(q=_rows(AT[5], 64, 0, 4)), B.LORA_ERR_INVALID_ARG),
+    (dict(H=AT[0], ldh=72), B.LORA_ERR_INVALID_ARG), (dict(Y=AT[1] + 128, R=AT[1]), B.LORA_ERR_INVALID_ARG), (dict(H=AT[4]), B.LORA_ERR_INVALID_ARG),
+    (dict(Y=AT[2]), B.LORA_ERR_INVALID_ARG), (dict(q=_rows(AT[0], 64, AT[6], 4)), B.LORA_ERR_INVALID_ARG),
+    (dict(q=_rows(AT[5], 64, AT[4] + 4, 4)), B.LORA_ERR_INVALID_ARG),
+])
+def test_norm_refusals(kw, status):
+    assert mx.lora_rms_norm(None, _norm(**kw), None, raw=True) == status
+
+
+def _plan(T=200, n_adapters=2, r_max=16):
+    p = B.lora_plan_t()
+    p.T, p.n_req, p.n_adapters, p.r_max, p.magic, p.unit_rows, p.scalars = T, 1, n_adapters, r_max, 0x4c6f5241, 16, AT[9]
+    return p
+
+
+def _linear(T=200, tbl=True, **kw):
+    table = B.make_adapter_table(2, AT[7], AT[7] + 64, AT[7] + 128)
+    f = dict(K=64, N=40, flags=0, reserved=0, X=AT[0], ldx=64, Xq=_rows(AT[1], 64, AT[2], 4), W=_rows(AT[3], 32, AT[4], 4, mx.LORA_MX_E2M1), Y=AT[5],
+             ldy=40, tbl=C.pointer(table) if tbl else None, ws=AT[6], wsb=1 << 30)
+    f.update(kw)
+    d = mx.lora_mx_linear_desc(*f.values())
+    d._keep = table
+    return d
+
+
+@pytest.mark.parametrize("T,kw,status", [
+    (200, dict(), B.LORA_ERR_INVALID_ARG),  # (all is well but the context)
+    (200, dict(flags=1), B.LORA_ERR_INVALID_ARG), (200, dict(reserved=1), B.LORA_ERR_INVALID_ARG), (200, dict(K=48), B.LORA_ERR_SHAPE),
+    (200, dict(K=0), B.LORA_ERR_SHAPE), (200, dict(N=0), B.LORA_ERR_SHAPE), (200, dict(ldx=56), B.LORA_ERR_SHAPE), (200, dict(ldy=32), B.LORA_ERR_SHAPE),
+    (200, dict(ldx=68), B.LORA_ERR_ALIGNMENT), (200, dict(ldy=44), B.LORA_ERR_ALIGNMENT), (200, dict(X=0), B.LORA_ERR_INVALID_ARG),
+    (200, dict(X=0, tbl=None, Xq=NOQ), B.LORA_ERR_INVALID_ARG), (200, dict(Y=0), B.LORA_ERR_INVALID_ARG), (200, dict(Y=AT[5] + 8), B.LORA_ERR_ALIGNMENT),
+    (200, dict(W=_rows(AT[3], 64, AT[4], 4)), B.LORA_ERR_INVALID_ARG), (200, dict(W=_rows(0, 32, AT[4], 4, 0)), B.LORA_ERR_INVALID_ARG),
+    (200, dict(W=_rows(AT[3], 16, AT[4], 4, 0)), B.LORA_ERR_SHAPE), (200, dict(W=_rows(AT[3], 1 << 24, AT[4], 4, 0)), B.LORA_ERR_SHAPE),
+    (200, dict(Xq=_rows(AT[1], 64, AT[2], 4, mx.LORA_MX_E2M1)), B.LORA_ERR_INVALID_ARG), (200, dict(Xq=_rows(AT[1], 1 << 26, AT[2], 4)), B.LORA_ERR_SHAPE),
+    (200, dict(ldx=1 << 24), B.LORA_ERR_SHAPE), (200, dict(ws=0), B.LORA_ERR_INVALID_ARG), (200, dict(ws=AT[6] + 16), B.LORA_ERR_ALIGNMENT),
+    (200, dict(wsb=100), B.LORA_ERR_WORKSPACE_TOO_SMALL), (200, dict(Y=AT[0] + 16), B.LORA_ERR_INVALID_ARG), (200, dict(Y=AT[1] + 16), B.LORA_ERR_INVALID_ARG),
+    (200, dict(Y=AT[3] + 16), B.LORA_ERR_INVALID_ARG), (200, dict(Y=AT[4]), B.LORA_ERR_INVALID_ARG), (200, dict(Y=AT[6] + 256), B.LORA_ERR_INVALID_ARG),
+    (200, dict(ws=AT[3]), B.LORA_ERR_INVALID_ARG), (20, dict(wsb=100), B.LORA_ERR_WORKSPACE_TOO_SMALL), (0, dict(Y=0, ws=0), B.LORA_ERR_INVALID_ARG),
+])
+def test_linear_refusals(T, kw, status):
+    d = _linear(**kw)
+    assert mx.lora_mx_linear(None, _plan(T), d, None, raw=True) == status
+    assert mx.lora_mx_linear_multi(None, _plan(T), [d], None, raw=True) == status
+
+
+def test_linear_needs_a_plan_and_a_table_that_fits_it():
+    d = _linear()
+    p = _plan()
+    p.magic = 1
+    assert mx.lora_mx_linear(None, p, d, None, raw=True) == B.LORA_ERR_PLAN
+    assert mx.lora_mx_linear(None, _plan(n_adapters=3), d, None, raw=True) == B.LORA_ERR_INVALID_ARG
+    assert mx.lib().lora_mx_linear_multi(None, C.byref(p), None, 1, None) == B.LORA_ERR_INVALID_ARG
+
+
+def test_multi_refusals():
+    p = _plan()
+    call = lambda *d: mx.lora_mx_linear_multi(None, p, list(d), None, raw=True)  # noqa: E731
+    other = dict(Y=AT[8], ws=AT[7] + (1 << 34))
+    assert call() == B.LORA_ERR_INVALID_ARG and call(*[_linear()] * 5) == B.LORA_ERR_INVALID_ARG
+    for kw in (dict(X=AT[0] + 16), dict(ldx=72), dict(Xq=_rows(AT[1] + 16, 64, AT[2], 4)), dict(Xq=NOQ), dict(Y=AT[5]), dict(ws=AT[6] + 256),
+               dict(Y=AT[5] + 16, ldy=40)):
+        assert call(_linear(), _linear(**{**other, **kw})) == B.LORA_ERR_INVALID_ARG
+
+
+def test_workspace_bytes():
+    f = mx.lora_mx_linear_workspace_bytes
+    assert f(-1, 64, 64, 8, 0) == f(1, 48, 64, 8, 0) == f(1, 64, 0, 8, 0) == f(1, 64, 64, -8, 0) == f(1, 64, 64, 8, 2) == 0
+    assert f(0, 64, 64, 0, 0) >= 256 and f(0, 64, 64, 0, 1) >= 256
+    for T in (1, 128, 129, 5000):
+        for xq in (0, 1):
+            least = B.lora_linear_workspace_bytes_preferred(T, 4096, 1000, 16, B.LORA_DTYPE_BF16)
+            assert f(T, 4096, 1000, 16, xq) >= least + (2 * 4096 * 1000 if T > 128 and not xq else 0)
+            assert f(T, 4096, 1000, 16, xq) % 256 == 0
+
+
+# ---- pins of the oracle: library types, and tables written by hand --------------------------------------------------------------
+
+def test_oracle_elements_are_the_formats():
+    torch = pytest.importorskip("torch")
+    codes = torch.arange(256, dtype=torch.uint8)
+    assert np.array_equal(ref.elements("e4m3"), codes.view(torch.float8_e4m3fn).double().numpy(), equal_nan=True)
+    assert list(ref.elements("e2m1")[:8]) == [0, 0.5, 1, 1.5, 2, 3, 4, 6] and ref.elements("e2m1")[9] == -0.5
+
+
+def test_oracle_quantize_by_hand():
+    x = np.zeros((3, 32))
+    x[0, :6] = [6.0, -0.25, 0.75, 1.25, -2.5, 5.0]  # scale 1; ties to the even code: 0, 1, 1, 2, 4
+    x[1, :2] = [6.001, 1.0]                          # just out of range: scale 2
+    x[2, :3] = [3.0, 1.5, 0.124]                     # scale 1/2: 6, 3, 0 (0.248 is below the tie)
+    codes, scales = ref.quantize(x, "e2m1")
+    assert list(scales[:, 0]) == [127, 128, 126]
+    v = ref.dequantize(codes, scales, "e2m1")
+    assert list(v[0, :6]) == [6, 0, 1, 1, -2, 4] and list(v[1, :2]) == [6, 1] and list(v[2, :3]) == [3, 1.5, 0]
+    assert codes[0, 0] == 0x87  # (6.0 in the low half, -0 above it)
+
+
+def test_oracle_quantize_matches_the_library_conversion():
+    torch = pytest.importorskip("torch")
+    x = np.random.default_rng(0).standard_normal((50, 64)) * 3
+    codes, scales = ref.quantize(x, "e4m3")
+    s = np.exp2(scales.astype(float) - 127)
+    amax = np.abs(x).reshape(50, 2, 32).max(-1)
+    assert (amax <= 448 * s).all() and (amax > 224 * s).all()
+    want = torch.from_numpy((x / np.repeat(s, 32, 1)).astype(np.float64)).to(torch.float32).to(torch.float8_e4m3fn)
+    assert np.array_equal(codes, want.view(torch.uint8).numpy())
+
+
+def test_oracle_norm_and_layer_closed_forms():
+    h, y = ref.rms_norm(np.array([[3.0, 4.0]]), np.array([1.0, 2.0]), 0.0, np.array([[0.0, 0.0]]))
+    assert np.allclose(y, [[3 / np.sqrt(12.5), 8 / np.sqrt(12.5)]]) and np.array_equal(h, [[3.0, 4.0]])
+    X, W, A, Bw = np.array([[1.0, 2.0], [3.0, 4.0]]), np.array([[1.0, -1.0]]), [np.array([[1.0, 1.0]])], [np.array([[2.0]])]
+    Y, S, D = ref.linear(X, W, X, [-1, 0], A, Bw, [0.5])
+    assert np.array_equal(Y, [[-1.0], [-1.0 + 0.5 * 7 * 2]]) and np.array_equal(S, [[3.0], [14.0]]) and np.array_equal(D, [[0.0], [7.0]])
