@@ -87,6 +87,8 @@ struct lora_ctx {
     int opt_plan_variant = -1;
     int opt_expand_split = -1;
     int opt_gemm_split_k = -1;
+    int opt_mx_tile = -1;
+    int opt_mx_split_k = -1;
     // profiling mode: event pairs recorded tightly around each kernel
     bool prof_on = false;
     int prof_cap = 0;
@@ -1200,6 +1202,12 @@ int lora_ctx_set_option(lora_ctx *ctx, const char *name, int value) {
     } else if (!strcmp(name, "plan_variant")) {
         if (value > 1) return LORA_ERR_INVALID_ARG;
         ctx->opt_plan_variant = value;
+    } else if (!strcmp(name, "mx_tile")) {
+        if (value >= kMxTileCount) return LORA_ERR_INVALID_ARG;
+        ctx->opt_mx_tile = value;
+    } else if (!strcmp(name, "mx_split_k")) {
+        if (value == 0 || value > 8) return LORA_ERR_INVALID_ARG;
+        ctx->opt_mx_split_k = value;
     } else if (!strcmp(name, "shrink_rank_block")) {
         if (value > 0 && value != 8 && value != 16 && value != 32 && value != 64) return LORA_ERR_INVALID_ARG;
         ctx->opt_shrink_rank_block = value;

@@ -94,6 +94,47 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_quantize_kernel(MxConvertArg
     }
 }
 
+// A bf16 row as the sum of two e4m3 rows: the first is the row's quantization, the second that of what it leaves, with a scale
+// 2^-4 of the first's (a remainder is at most half a step of the first, 2^-4 of 256 .. 448 there).  bf16 has 8 significant bits and each
+// part holds 4, so the sum is the value itself where the second part's smallest step, 2^-13 of the first scale, is not above the
+// value's own -- down to 2^-14 of its block's largest -- and off by at most 2^-22 of that largest value below.
+__global__ __launch_bounds__(kMxWaves * 64) void mx_split_kernel(MxSplitArgs p) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned unit = blockIdx.x * kMxWaves + wave, urow = unit / (unsigned)p.strips;
+    if (urow >= (unsigned)p.rows) return;
+    const int k0 = (int)(unit - urow * p.strips) * kMxStrip + lane * 8;
+    const __bf16 *src = static_cast<const __bf16 *>(p.X) + (int64_t)urow * p.ldx;
+    unsigned char *codes = p.codes + (int64_t)urow * 2 * p.part_bytes, *scales = p.scales + (int64_t)urow * 2 * p.part_scales;
+    float v[kMxPieces][8];
+#pragma unroll
+    for (int i = 0; i < kMxPieces; ++i) load8(src + min(k0 + i * 512, p.K - 8), v[i]);
+#pragma unroll
+    for (int i = 0; i < kMxPieces; ++i) {
+        const int k = k0 + i * 512;
+        const int s = scale_code<kMxE4M3>(quad_max(v[i])), s2 = s == 255 ? 255 : max(s - 4, 0);
+        const float inv = inverse_scale(s), up = s == 255 ? 1.f : __uint_as_float((unsigned)(127 + s - s2) << 23);
+        uint2 hi = codes_e4m3(v[i], inv), lo;
+        float r[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned c = h ? hi.y : hi.x;
+            const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
+            const float back[4] = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[h * 4 + e] = v[i][h * 4 + e] * inv - back[e];
+        }
+        lo = codes_e4m3(r, up);
+        if (k >= p.part_bytes) continue;
+        if (k >= p.K) hi = lo = make_uint2(0u, 0u);
+        *reinterpret_cast<uint2 *>(codes + k) = hi;
+        *reinterpret_cast<uint2 *>(codes + p.part_bytes + k) = lo;
+        if ((lane & 3) == 0) {
+            scales[k >> 5] = (unsigned char)s;
+            scales[p.part_scales + (k >> 5)] = (unsigned char)s2;
+        }
+    }
+}
+
 __device__ __forceinline__ void store_values(__bf16 *dst, const float (&v)[8]) { store8(dst, v); }
 __device__ __forceinline__ void store_values(float *dst, const float (&v)[8]) { store8(dst, v); }
 
@@ -273,6 +314,15 @@ hipError_t launch_mx_dequantize(const MxConvertArgs &a, int dtype, int format, h
         return format == kMxE2M1 ? launch_kernel(mx_dequantize_kernel<float, kMxE2M1>, grid, block, 0, stream, timer, b)
                                  : launch_kernel(mx_dequantize_kernel<float, kMxE4M3>, grid, block, 0, stream, timer, b);
     });
+}
+
+hipError_t launch_mx_split(const MxSplitArgs &a0, hipStream_t stream, const KernelTimer *timer) {
+    MxSplitArgs a = a0;
+    a.strips = (a.part_bytes + kMxStrip - 1) / kMxStrip;
+    const int64_t units = (int64_t)a.rows * a.strips;
+    if (units <= 0) return hipSuccess;
+    if (units > INT32_MAX || a.part_bytes % 512 || a.part_bytes < a.K || a.part_scales < a.part_bytes / kMxBlock) return hipErrorInvalidValue;
+    return launch_kernel(mx_split_kernel, dim3((unsigned)((units + kMxWaves - 1) / kMxWaves)), dim3(kMxWaves * 64), 0, stream, timer, a);
 }
 
 hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, int num_cu, hipStream_t stream, const KernelTimer *timer) {

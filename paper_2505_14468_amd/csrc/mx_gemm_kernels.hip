@@ -1,11 +1,34 @@
-// Tiled product of a 4-bit backbone and 8-bit activations, both with a scale for every 32 values:
+// Tiled product of a 4-bit backbone and 8-bit activations, both with a scale for every 32 values, with the LoRA expand behind it:
 //
-//     Y[row, n] = sum_k X[row, k] W[n, k]  (+ D[row, n] for rows with an adapter),   rounded once
+//     Y[row, n] = sum_k X[row, k] W[n, k]  +  sum_j V[row, j] B_a[n, j]  (+ D[row, n]),   row = perm[slot], rounded once
 //
-// on the block-scaled matrix instructions: one 16x16x128 MFMA takes 128 values of 16 rows of W (e2m1) and of 16 rows of X
-// (e4m3) with the scales of their blocks, so nothing is ever taken apart.  Of a 16-row operand of W, lane l holds block l / 16
-// of row l % 16 (16 bytes); of X the 16-byte pieces l / 16 and 4 + l / 16 of the row's 128 bytes (measured: element e of lane
-// group g is value 16 g + e for e < 16, 48 + 16 g + e behind); a scale operand is block l / 16's of row l % 16 for both.
+// The base product runs on the block-scaled matrix instructions: one 16x16x128 MFMA takes 128 values of 16 rows of W (e2m1) and of
+// 16 rows of X (e4m3) with the scales of their blocks, so nothing is ever taken apart.  Of a 16-row operand of W, lane l holds
+// block l / 16 of row l % 16 (16 bytes); of X the 16-byte pieces l / 16 and 4 + l / 16 of the row's 128 bytes (measured: element e
+// of lane group g is value 16 g + e for e < 16, 48 + 16 g + e behind); the scale operand is that of block l / 16 for both, one byte
+// of a register that holds four.
+//
+// Activations of PARTS == 2 come as the sum of two sets of 8-bit values (a bf16 row taken apart, mx_split_kernel): the
+// contraction axis is walked twice, once for each, against the same W.
+//
+// Tile: BM rows x BN columns, stages of 128 values of the contraction axis, two of them in LDS, loaded there directly.  4
+// waves, one per SIMD, each a quarter of the tile.  What a stage costs a wave besides its MFMAs (256 x 256: 64 of them, 32
+// cycles each) is 24 operand reads, 12 loads and a few scalar instructions, dealt out one behind an MFMA; the scales cost
+// nothing there: of four stages together they are read once, in the order that the instruction wants them (below).
+//
+// The wave's tile is cut into halves along both sides, W0 W1 and X0 X1; a stage multiplies its four quadrants in the order
+//     (W0, Xa) (W0, Xb) | barrier | (W1, Xb) (W1, Xa)         a = 0, b = 1 in even stages, the reverse in odd ones
+// so that every half of the operands is free a quadrant before the next stage's takes its registers: Xb and W1 are read from LDS
+// during the first quadrant, W0 of the next stage during the third, its first X half (this one's Xb) during the fourth.
+// The one barrier of a stage therefore stands where all of the stage has been read: its LDS takes the stage after next at once,
+// which then has a whole stage to arrive, and the next one has arrived.
+//
+// The extension runs behind the base product on bf16 16x16x32 MFMAs, segment by segment (the rows of a tile are in slot order, so
+// an adapter's are contiguous), with operands straight from memory: a few k-steps per tile, against K / 128 stages.  Rows of others
+// in a 16-row block meet zeros of V.
+#include <type_traits>
+#include <utility>
+
 #include "mx_kernels.h"
 
 namespace lora {
@@ -15,22 +38,85 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ unsigned load_u32(const void *p) { return *(const __attribute__((address_space(1))) unsigned *)p; }
 
-// LDS position (in 16-byte pieces) of piece c of row r: rows of X of 8 pieces, rows of W of 4, two to a line of 8.
+template <int A, typename F, int... I>
+__device__ __forceinline__ void for_impl(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, A + I>{}), ...);
+}
+template <int A, int B, typename F>
+__device__ __forceinline__ void for_each(F &&f) {
+    for_impl<A>(f, std::make_integer_sequence<int, (B > A ? B - A : 0)>{});
+}
+
+// LDS position (in 16-byte pieces) of piece c of row r: rows of X of 8 pieces, rows of W of 4, two to a line of 8.  16 rows of one
+// piece column, as an operand read takes them, then lie in 16 different quarters of the banks.
 __device__ __forceinline__ int x_at(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
 __device__ __forceinline__ int w_at(int r, int c) { return (r >> 1) * 8 + ((((r & 1) << 2) | c) ^ ((r >> 2) & 3)); }
 
-template <int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN * 64) void mx_gemm_kernel(MxGemmArgs p, int tiles_m, int tiles_n, int group_m) {
-    constexpr int NT = WM * WN * 64;
-    constexpr int WTM = BM / WM, WTN = BN / WN, NBT = WTM / 16, NBN = WTN / 16;
-    constexpr int XL = BM * 8 / NT, WL = BN * 4 / NT;
-    static_assert(XL * NT == BM * 8 && WL * NT == BN * 4 && BM + BN <= NT * 2 && NBN % 2 == 0, "tile and workgroup");
-    __shared__ __attribute__((aligned(16))) chunk_t sX[BM * 8];
-    __shared__ __attribute__((aligned(16))) chunk_t sW[BN * 4];
-    __shared__ unsigned sS[BM + BN];
-    __shared__ int srow[BM];
-    __shared__ unsigned char use_d[BM];
+// acc += W X on byte S of the scale registers, in place.  Assembly for the reason that Elem<>::mma_step gives: the accumulators
+// stay in their registers; mma_settle keeps the distance to whatever touches them next.
+template <int S>
+__device__ __forceinline__ void mma_scaled(f32x4_t &acc, const u32x4_t &w, const i32x8_t &x, unsigned ws, unsigned xs) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (S == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4" : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+    else if constexpr (S == 1)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4" : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+    else if constexpr (S == 2)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,1,0] cbsz:4" : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+    else
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[1,1,0] cbsz:4" : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+#else
+    (void)acc, (void)w, (void)x, (void)ws, (void)xs;
+#endif
+}
 
+// The scales of 16 blocks of a row (a superstage: four stages of four blocks), as the four dwords that hold byte g of each stage.
+__device__ __forceinline__ chunk_t transpose_scales(const chunk_t &d) {
+    const unsigned a = __builtin_amdgcn_perm(d.y, d.x, 0x05010400u), b = __builtin_amdgcn_perm(d.y, d.x, 0x07030602u);
+    const unsigned c = __builtin_amdgcn_perm(d.w, d.z, 0x05010400u), e = __builtin_amdgcn_perm(d.w, d.z, 0x07030602u);
+    return make_uint4(__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u), __builtin_amdgcn_perm(e, b, 0x05040100u),
+                      __builtin_amdgcn_perm(e, b, 0x07060302u));
+}
+// Scales of blocks 16 s .. 16 s + 15 of a row of n (zeros past it).
+__device__ __forceinline__ chunk_t load_scales(const unsigned char *row, int s, int n) {
+    if (s * 16 + 16 <= n) {  // (4-byte alignment is enough)
+        typedef u32x4_t u32x4_4_t __attribute__((aligned(4)));
+        const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_4_t *)(row + s * 16);
+        return make_uint4(v.x, v.y, v.z, v.w);
+    }
+    unsigned d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = n - s * 16 - i * 4;  // blocks in this dword
+        d[i] = load_u32(row + (left > 0 ? s * 16 + i * 4 : 0));
+        d[i] &= left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1u : 0u;
+    }
+    return make_uint4(d[0], d[1], d[2], d[3]);
+}
+
+template <int BM, int BN>
+struct MxTile {
+    static constexpr int NT = 256, WTM = BM / 2, WTN = BN / 2, NBT = WTM / 16, NBN = WTN / 16, HT = NBT / 2, HN = NBN / 2;
+    static constexpr int GX = BM / 32, GW = BN / 64;  // direct loads of a stage per wave
+    static constexpr size_t x_bytes = (size_t)BM * 128, w_bytes = (size_t)BN * 64, s_bytes = (size_t)(BM + BN) * 16;
+    static constexpr size_t smem = 2 * (x_bytes + w_bytes + s_bytes) + (size_t)BM * 5;
+    static_assert(NBT % 2 == 0 && NBN % 2 == 0 && HT >= 1 && HN >= 1 && GX >= 1 && GW >= 1 && BM + BN <= 2 * NT && BM <= NT && BN <= NT, "tile shape");
+};
+
+template <int BM, int BN, int PARTS, bool SPLIT>
+__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m, int tiles_n, int group_m) {
+    typedef MxTile<BM, BN> M;
+    typedef __bf16 E;
+    constexpr int NBT = M::NBT, NBN = M::NBN, HT = M::HT, HN = M::HN, GX = M::GX, GW = M::GW;
+
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    chunk_t *sX = reinterpret_cast<chunk_t *>(smem);                             // [2][BM * 8]
+    chunk_t *sW = reinterpret_cast<chunk_t *>(smem + 2 * M::x_bytes);            // [2][BN * 4]
+    chunk_t *sS = reinterpret_cast<chunk_t *>(smem + 2 * (M::x_bytes + M::w_bytes));  // [2][BM + BN], a superstage each
+    int *srow = reinterpret_cast<int *>(sS + 2 * (BM + BN));                     // tile row -> original row
+    unsigned char *use_d = reinterpret_cast<unsigned char *>(srow + BM);         // tile row takes its adapter term from D
+
+    // ---- workgroup -> tile: consecutive ids go round the 8 XCDs, each walks a contiguous, M-grouped range ----
     const int total = tiles_m * tiles_n;
     const int per_xcd = (total + 7) >> 3;
     const int lin = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
@@ -44,105 +130,336 @@ __global__ __launch_bounds__(WM *WN * 64) void mx_gemm_kernel(MxGemmArgs p, int 
     const MxGemmSet g = p.set[si];
     const int m0 = pm * BM, n0 = (pn - g.tile0) * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wn0 = (wave % WN) * WTN, wm0 = (wave / WN) * WTM;
+    const int wn0 = (wave & 1) * M::WTN, wm0 = (wave >> 1) * M::WTM;
     const int lr = lane & 15, lq = lane >> 4;
-    if (p.plan.scalars[kScStatus] != 0) return;
-    for (int r = tid; r < BM; r += NT) {
-        const int t = min(m0 + r, p.T - 1);
-        srow[r] = t;
-        use_d[r] = g.D != nullptr && p.plan.row_adapter[t] >= 0;
+
+    // this workgroup's stretch of the contraction axis, in blocks of 32 and stages of four
+    const int nblocks = p.K / kMxBlock;
+    int b0 = 0, nloc = nblocks;
+    if constexpr (SPLIT) {
+        b0 = (int)blockIdx.y * p.chunk_blocks;
+        nloc = min(nblocks - b0, p.chunk_blocks);
     }
-    const int nblocks = p.K / kMxBlock, KT = (nblocks + 3) / 4;
+    // Stages of one part.  (Two parts: whole superstages -- the rows of X are that long and hold zeros past K.)
+    const int KP = PARTS == 2 ? (nloc + 15) >> 4 << 2 : (nloc + 3) >> 2;
+    const int KT = KP * PARTS;
+
+    // ---- what is loaded where -------------------------------------------------------------------------------------
+    const int rx0 = wave * GX * 8, rw0 = wave * GW * 16;  // first tile row of the wave's loads
+    int orig[GX];
+#pragma unroll
+    for (int i = 0; i < GX; ++i) orig[i] = p.plan.perm[min(m0 + rx0 + i * 8 + (lane >> 3), p.T - 1)];
+    const int my_row = p.plan.perm[min(m0 + tid % BM, p.T - 1)];
+    const int status = p.plan.scalars[kScStatus];
+#pragma unroll
+    for (int i = 0; i < GX; ++i) asm volatile("" ::"v"(orig[i]));
+    if (status != 0) return;  // (a plan that was not built: its rows are whatever the buffer holds)
+    if (tid < BM) srow[tid] = my_row;
+    // 32-bit byte offsets, X's from its start, W's from the tile's first row; both descriptors end with the last row's last block
+    unsigned ox[GX], ow[GW];
+#pragma unroll
+    for (int i = 0; i < GX; ++i) {
+        const int row = rx0 + i * 8 + (lane >> 3);
+        ox[i] = (unsigned)((int64_t)orig[i] * p.ldxq) + (unsigned)((lane & 7) ^ ((row >> 1) & 7)) * 16u;
+    }
+#pragma unroll
+    for (int i = 0; i < GW; ++i) {
+        const int row = rw0 + i * 16 + 2 * (lane >> 3) + ((lane & 7) >> 2);
+        ow[i] = (unsigned)((int64_t)(min(n0 + row, g.N - 1) - n0) * g.ldwq) + (unsigned)((lane & 3) ^ ((row >> 2) & 3)) * 16u;
+    }
+    const unsigned char *Xb = p.Xq + (int64_t)b0 * 32, *Wb = g.Wq + (int64_t)n0 * g.ldwq + b0 * 16;
+    const int64_t x_row = PARTS == 2 ? 2 * (int64_t)p.part_bytes : (int64_t)nblocks * 32;  // bytes of a row of X in use
+    const int x_range = (int)(unsigned)((int64_t)(p.T - 1) * p.ldxq + x_row - (int64_t)b0 * 32);
+    const int w_range = (int)(unsigned)((int64_t)(min(BN, g.N - n0) - 1) * g.ldwq + (int64_t)(nblocks - b0) * 16);
+    const unsigned dx = lds_address(sX) + rx0 * 128, dw = lds_address(sW) + rw0 * 64;
+    BufferDesc Xd, Wd;
+    int x_so = 0, w_so = 0;
+    // (loads past the last stage are issued all the same, against descriptors of no bytes)
+    auto stage_desc = [&](int kt) __attribute__((always_inline)) {
+        int live;
+        asm("s_sub_i32 %0, %1, %2\n\ts_ashr_i32 %0, %0, 31" : "=s"(live) : "s"(kt), "s"(KT) : "scc");
+        Xd = make_buffer_desc(Xb, x_range & live);
+        Wd = make_buffer_desc(Wb, w_range & live);
+        if constexpr (PARTS == 1) {
+            x_so = __builtin_amdgcn_readfirstlane(kt * 128);
+            w_so = __builtin_amdgcn_readfirstlane(kt * 64);
+        } else {
+            const int part = kt >= KP ? 1 : 0, k = kt - (part ? KP : 0);
+            x_so = __builtin_amdgcn_readfirstlane(part * p.part_bytes + k * 128);
+            w_so = __builtin_amdgcn_readfirstlane(k * 64);
+        }
+    };
+    auto load_base = [&](auto jc, int buf) __attribute__((always_inline)) {
+        constexpr int j = jc.value;
+        if constexpr (j < GX)
+            set_lds_base<j * 1024>(dx + buf * (int)M::x_bytes);
+        else
+            set_lds_base<(j - GX) * 1024>(dw + buf * (int)M::w_bytes);
+    };
+    auto load = [&](auto jc) __attribute__((always_inline)) {
+        constexpr int j = jc.value;
+        if constexpr (j < GX)
+            load_to_lds(Xd, ox[j], x_so);
+        else
+            load_to_lds(Wd, ow[j - GX], w_so);
+    };
+    // ---- scales: thread t takes row t of W's tile and row t of X's; a superstage of both parts has the same of W -----------
+    const unsigned char *xs_row = p.Xs + (int64_t)my_row * p.ldxs + b0, *ws_row = g.Ws + (int64_t)min(n0 + tid % BN, g.N - 1) * g.ldws + b0;
+    const int SP = (KP + 3) >> 2;  // superstages of a part
+    chunk_t xs_new, ws_new;
+    auto request_scales = [&](int s) __attribute__((always_inline)) {
+        int k = s, part = 0;
+        if constexpr (PARTS == 2) part = s >= SP ? 1 : 0, k = s - (part ? SP : 0);
+        xs_new = load_scales(xs_row + part * p.part_scales, k, nloc);
+        ws_new = load_scales(ws_row, k, nloc);
+    };
+    auto store_scales = [&](int s) __attribute__((always_inline)) {
+        chunk_t *to = sS + (s & 1) * (BM + BN);
+        if (tid < BM) to[tid] = transpose_scales(xs_new);
+        if (tid < BN) to[BM + tid] = transpose_scales(ws_new);
+    };
+    request_scales(0);
+    for_each<0, 2>([&](auto sc) __attribute__((always_inline)) {
+        stage_desc(sc.value);
+        for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, sc.value), wait_state(), load(jc); });
+    });
+
+    // ---- which rows take their adapter term from D (short segments', when the long ones' is computed here) ---------------
+    if (g.D != nullptr && tid < BM) {
+        const int s = p.plan.row_seg[min(m0 + tid, p.T - 1)];
+        const bool lng = g.long_rows > 0 && p.plan.seg_indptr[s + 1] - p.plan.seg_indptr[s] >= g.long_rows;
+        use_d[tid] = p.plan.seg_adapter[s] >= 0 && !lng;
+    }
+
     f32x4_t acc[NBN][NBT];
 #pragma unroll
     for (int nb = 0; nb < NBN; ++nb)
 #pragma unroll
         for (int tb = 0; tb < NBT; ++tb) acc[nb][tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int kt = 0; kt < KT; ++kt) {
-        chunk_t xr[XL], wr[WL];
-        unsigned sr[2] = {0u, 0u};
+    auto settle = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < XL; ++i) {
-            const int idx = tid + i * NT, r = idx >> 3, c = kt * 8 + (idx & 7);
-            xr[i] = load_chunk(p.Xq + (int64_t)min(m0 + r, p.T - 1) * p.ldxq + min(c, nblocks * 2 - 1) * 16);
-            xr[i] = keep_if(c < nblocks * 2, xr[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < WL; ++i) {
-            const int idx = tid + i * NT, r = idx >> 2, c = kt * 4 + (idx & 3);
-            wr[i] = load_chunk(g.Wq + (int64_t)min(n0 + r, g.N - 1) * g.ldwq + min(c, nblocks - 1) * 16);
-        }
-        const unsigned live = nblocks - kt * 4 >= 4 ? ~0u : (1u << 8 * (nblocks - kt * 4)) - 1u;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = tid + i * NT;
-            if (r < BM)
-                sr[i] = load_u32(p.Xs + (int64_t)min(m0 + r, p.T - 1) * p.ldxs + kt * 4) & live;
-            else if (r < BM + BN)
-                sr[i] = load_u32(g.Ws + (int64_t)min(n0 + r - BM, g.N - 1) * g.ldws + kt * 4) & live;
-        }
+        for (int nb = 0; nb < NBN; ++nb) mma_settle(acc[nb]);
+    };
+    settle();
+
+    // What lies past K in the last stage of a part, once it is there: zeros in X (its codes are other bytes of memory, which may
+    // mean NaN; W's always mean something finite, and its scales are zeros there, 2^-127).
+    const int tail = PARTS == 1 ? nloc & 3 : 0;
+    auto zero_tail = [&](int buf) __attribute__((always_inline)) {
+        for (int i = tid; i < BM * 8; i += 256)
+            if ((i & 7) >= 2 * tail) sX[buf * BM * 8 + x_at(i >> 3, i & 7)] = zero_chunk();
         __syncthreads();
+    };
+    auto is_tail = [&](int kt) { return tail != 0 && kt == KT - 1; };
+
+    // ---- base product ---------------------------------------------------------------------------------------------------
+    {
+        u32x4_t w[2][HN];
+        i32x8_t x[2][HT];
+        unsigned wsc[2][HN], xsc[2][HT];
+        const chunk_t *px0 = sX + x_at(wm0 + lr, lq), *px1 = sX + x_at(wm0 + lr, 4 + lq), *pw = sW + w_at(wn0 + lr, lq);
+        const unsigned *psx = reinterpret_cast<const unsigned *>(sS) + (wm0 + lr) * 4 + lq, *psw = reinterpret_cast<const unsigned *>(sS) + (BM + wn0 + lr) * 4 + lq;
+        auto read_w = [&](int half, int i, int buf) __attribute__((always_inline)) {
+            w[half][i] = __builtin_bit_cast(u32x4_t, pw[buf * BN * 4 + (half * HN + i) * 64]);
+        };
+        auto read_x = [&](int half, int i, int part, int buf) __attribute__((always_inline)) {
+            const u32x4_t v = __builtin_bit_cast(u32x4_t, (part ? px1 : px0)[buf * BM * 8 + (half * HT + i) * 128]);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) {
-            const int idx = tid + i * NT;
-            sX[x_at(idx >> 3, idx & 7)] = xr[i];
-        }
+            for (int e = 0; e < 4; ++e) x[half][i][part * 4 + e] = (int)v[e];
+        };
+        auto read_ws = [&](int half, int i, int sbuf) __attribute__((always_inline)) { wsc[half][i] = psw[sbuf * (BM + BN) * 4 + (half * HN + i) * 64]; };
+        auto read_xs = [&](int half, int i, int sbuf) __attribute__((always_inline)) { xsc[half][i] = psx[sbuf * (BM + BN) * 4 + (half * HT + i) * 64]; };
+        auto pin = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+        constexpr int Q = HN * HT, GL = GX + GW;
+        constexpr auto load_slot = [](int j) { return (2 * j + 2) * 2 * Q / (2 * GL + 1); };
+        static_assert(load_slot(0) >= 1 && load_slot(GL - 1) < 2 * Q && 2 * Q > GL, "every load behind an MFMA of its own, none behind the first");
+        // Quadrant (half wh of W, half xh of X) on byte S of the scales; `beside(i)` is issued behind MFMA i.
+        auto quadrant = [&](auto sc, int wh, int xh, auto beside) __attribute__((always_inline)) {
+            for_each<0, Q>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = ic.value, nb = i / HT, tb = nb % 2 ? HT - 1 - i % HT : i % HT;
+                mma_scaled<sc.value>(acc[wh * HN + nb][xh * HT + tb], w[wh][nb], x[xh][tb], wsc[wh][nb], xsc[xh][tb]);
+                pin();
+                beside(ic);
+                pin();
+            });
+        };
+        auto stage = [&](int kt, int sbuf, auto sc) __attribute__((always_inline)) {
+            constexpr int s = sc.value, buf = s & 1, a = s & 1, b = a ^ 1;
+            // first quadrant: the other halves of this stage, X's first
+            quadrant(sc, 0, a, [&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = ic.value, R = 2 * HT + HN;
+                for_each<i * R / Q, (i + 1) * R / Q>([&](auto jc) __attribute__((always_inline)) {
+                    constexpr int j = jc.value;
+                    if constexpr (j < 2 * HT) {
+                        read_x(b, j / 2, j % 2, buf);
+                        if constexpr (s == 0 && j % 2 == 0) read_xs(b, j / 2, sbuf);
+                    } else {
+                        read_w(1, j - 2 * HT, buf);
+                        if constexpr (s == 0) read_ws(1, j - 2 * HT, sbuf);
+                    }
+                });
+            });
+            stage_desc(kt + 2);
+            quadrant(sc, 0, b, [&](auto) __attribute__((always_inline)) {});
+            wait_vm_barrier<0>();  // the next stage is there; this one has been read by every wave
+            if (is_tail(kt + 1)) zero_tail(buf ^ 1);
+            if constexpr (s == 0) {
+                if (kt + 4 < KT) request_scales((kt >> 2) + 1);
+            }
+            if constexpr (s == 1) {
+                if (kt + 3 < KT) store_scales((kt >> 2) + 1);  // (read from stage 3 on; its buffer was last read in the stage before this)
+            }
+            // third and fourth quadrant: W0, then Xb of the next stage; the stage after next is requested
+            auto loads = [&](auto ic) __attribute__((always_inline)) {  // (i: of 2 Q MFMAs; where a load goes is set one MFMA ahead)
+                constexpr int i = ic.value;
+                for_each<0, GL>([&](auto jc) __attribute__((always_inline)) {
+                    if constexpr (load_slot(jc.value) == i) load(jc);
+                });
+                for_each<0, GL>([&](auto jc) __attribute__((always_inline)) {
+                    if constexpr (load_slot(jc.value) == i + 1) load_base(jc, buf);
+                });
+            };
+            quadrant(sc, 1, b, [&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = ic.value;
+                for_each<i * HN / Q, (i + 1) * HN / Q>([&](auto jc) __attribute__((always_inline)) {
+                    read_w(0, jc.value, buf ^ 1);
+                    if constexpr (s == 3) read_ws(0, jc.value, sbuf ^ 1);
+                });
+                loads(ic);
+            });
+            quadrant(sc, 1, a, [&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = ic.value;
+                for_each<i * 2 * HT / Q, (i + 1) * 2 * HT / Q>([&](auto jc) __attribute__((always_inline)) {
+                    read_x(b, jc.value / 2, jc.value % 2, buf ^ 1);
+                    if constexpr (s == 3 && jc.value % 2 == 0) read_xs(b, jc.value / 2, sbuf ^ 1);
+                });
+                loads(std::integral_constant<int, i + Q>{});
+            });
+        };
+        store_scales(0);
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what is loaded in front of the loop has arrived, and the compiler knows
+        wait_vm_barrier<0>();
+        if (is_tail(0)) zero_tail(0);
 #pragma unroll
-        for (int i = 0; i < WL; ++i) {
-            const int idx = tid + i * NT;
-            sW[w_at(idx >> 2, idx & 3)] = wr[i];
-        }
+        for (int i = 0; i < HN; ++i) read_w(0, i, 0), read_ws(0, i, 0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (tid + i * NT < BM + BN) sS[tid + i * NT] = sr[i];
-        __syncthreads();
-        i32x8_t x[NBT];
-        int xsc[NBT];
-#pragma unroll
-        for (int tb = 0; tb < NBT; ++tb) {
-            const int r = wm0 + tb * 16 + lr;
-            const chunk_t a = sX[x_at(r, lq)], b = sX[x_at(r, 4 + lq)];
-            x[tb] = i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
-            xsc[tb] = (int)(sS[r] >> (8 * lq));
-        }
-#pragma unroll
-        for (int nb = 0; nb < NBN; ++nb) {
-            const int r = wn0 + nb * 16 + lr;
-            const chunk_t a = sW[w_at(r, lq)];
-            const i32x8_t w{(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
-            const int wsc = (int)(sS[BM + r] >> (8 * lq));
-#pragma unroll
-            for (int tb = 0; tb < NBT; ++tb)
-                acc[nb][tb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[tb], acc[nb][tb], 4, 0, 0, wsc, 0, xsc[tb]);
+        for (int i = 0; i < HT; ++i) read_x(0, i, 0, 0), read_x(0, i, 1, 0), read_xs(0, i, 0);
+#pragma clang loop unroll(disable)
+        for (int kt = 0; kt < KT; kt += 4) {
+            const int sbuf = (kt >> 2) & 1;
+            stage(kt, sbuf, std::integral_constant<int, 0>{});
+            if (kt + 1 >= KT) break;
+            stage(kt + 1, sbuf, std::integral_constant<int, 1>{});
+            if (kt + 2 >= KT) break;
+            stage(kt + 2, sbuf, std::integral_constant<int, 2>{});
+            if (kt + 3 >= KT) break;
+            stage(kt + 3, sbuf, std::integral_constant<int, 3>{});
         }
     }
-    const int pc = n0 + wn0 + pair_column(lane);
-    __bf16 *Y = static_cast<__bf16 *>(g.Y);
-#pragma unroll
-    for (int tb = 0; tb < NBT; ++tb) {
-        const int t = wm0 + tb * 16 + lr;
-        const bool ok = m0 + t < p.T, has = use_d[t] != 0;
-#pragma unroll
-        for (int i = 0; i < NBN / 2; ++i) {
-            float v[8];
-            pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
-            const int n = pc + i * 32;
-            if (has) {
-                float d[8];
-                const float *src = g.D + (int64_t)srow[t] * g.ldd + min(n, (int)g.ldd - 8);
-                const chunk_t a = load_chunk(src), b = load_chunk(src + 4);
-                d[0] = __uint_as_float(a.x), d[1] = __uint_as_float(a.y), d[2] = __uint_as_float(a.z), d[3] = __uint_as_float(a.w);
-                d[4] = __uint_as_float(b.x), d[5] = __uint_as_float(b.y), d[6] = __uint_as_float(b.z), d[7] = __uint_as_float(b.w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += d[e];
+    settle();
+    wait_vm<0>();  // (loads past the end: none may arrive in LDS that is another workgroup's by then)
+
+    // ---- extension --------------------------------------------------------------------------------------------------------
+    if (!SPLIT && g.B != nullptr) {
+        const E *V = static_cast<const E *>(g.V);
+        const int m_end = min(m0 + BM, p.T);
+        const int s_first = p.plan.row_seg[m0], s_last = p.plan.row_seg[m_end - 1];
+        for (int s = s_first; s <= s_last; ++s) {
+            const int lo = p.plan.seg_indptr[s], hi = p.plan.seg_indptr[s + 1], ad = p.plan.seg_adapter[s], r = p.plan.seg_rank[s];
+            if (ad < 0 || r <= 0 || hi - lo < g.long_rows) continue;
+            const E *Ba = static_cast<const E *>(g.B[ad]);
+            if (Ba == nullptr) {
+                if (tid == 0) atomicMin(&p.plan.scalars[kScEvicted], kErrNotResident);  // slot emptied after the plan
+                continue;
             }
-            if (ok) store_columns(Y + (int64_t)srow[t] * g.ldy, n, g.N, v);
+            const int tlo = max(lo - m0, 0), thi = min(hi - m0, BM);  // tile rows of the segment
+            if (thi <= wm0 || tlo >= wm0 + M::WTM) continue;
+            for (int j0 = 0; j0 < r; j0 += 32) {
+                const int j = j0 + lq * 8;
+                const bool jok = j < r;
+                chunk_t wv[NBN], xv[NBT];
+#pragma unroll
+                for (int nb = 0; nb < NBN; ++nb) wv[nb] = load_chunk(Ba + (int64_t)min(n0 + wn0 + nb * 16 + lr, g.N - 1) * r + (jok ? j : 0));
+#pragma unroll
+                for (int tb = 0; tb < NBT; ++tb) xv[tb] = load_chunk(V + (int64_t)srow[wm0 + tb * 16 + lr] * p.r_max + (jok ? j : 0));
+#pragma unroll
+                for (int nb = 0; nb < NBN; ++nb) wv[nb] = keep_if(jok, wv[nb]);
+#pragma unroll
+                for (int tb = 0; tb < NBT; ++tb) {
+                    const int t = wm0 + tb * 16 + lr;
+                    xv[tb] = keep_if(jok && t >= tlo && t < thi, xv[tb]);
+                }
+                operand_settle(wv);
+                operand_settle(xv);
+#pragma unroll
+                for (int tb = 0; tb < NBT; ++tb) {
+                    const int t0 = wm0 + tb * 16;
+                    if (tlo < t0 + 16 && thi > t0) {
+#pragma unroll
+                        for (int nb = 0; nb < NBN; ++nb) Elem<E>::mma_step(acc[nb][tb], wv[nb], xv[tb], 0);
+                    }
+                }
+            }
+        }
+        settle();
+    }
+
+    // ---- the single store of Y (or of a split's partial sums, in fp32) -----------------------------------------------------
+    constexpr int NP = NBN / 2;
+    const int pc = n0 + wn0 + pair_column(lane);
+    if constexpr (SPLIT) {
+        float *P = p.P + (int64_t)blockIdx.y * p.T * p.ldp;
+#pragma unroll
+        for (int tb = 0; tb < NBT; ++tb) {
+            const int t = wm0 + tb * 16 + lr;
+            float *prow = P + (int64_t)srow[t] * p.ldp;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float v[8];
+                pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
+                if (m0 + t < p.T) store_columns(prow, pc + i * 32, g.N, v);
+            }
+        }
+    } else {
+        E *Y = static_cast<E *>(g.Y);
+        chunk_t term[2][2 * NP];
+        auto fetch = [&](int tb, chunk_t(&d)[2 * NP]) __attribute__((always_inline)) {
+            const int t = wm0 + tb * 16 + lr;
+            const float *drow = g.D + (use_d[t] != 0 ? (int64_t)srow[t] * g.ldd : 0);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const float *src = drow + min(pc + i * 32, (int)g.ldd - 8);  // (columns past N: loaded, never stored)
+                d[2 * i] = load_chunk(src);
+                d[2 * i + 1] = load_chunk(src + 4);
+            }
+        };
+        if (g.D != nullptr) fetch(0, term[0]);
+#pragma unroll
+        for (int tb = 0; tb < NBT; ++tb) {
+            const int t = wm0 + tb * 16 + lr;
+            const bool ok = m0 + t < p.T, has = g.D != nullptr && use_d[t] != 0;
+            E *yrow = Y + (int64_t)srow[t] * g.ldy;
+            if (g.D != nullptr && tb + 1 < NBT) fetch(tb + 1, term[(tb + 1) & 1]);  // (a block ahead of the stores)
+            const chunk_t(&d)[2 * NP] = term[tb & 1];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float v[8];
+                pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
+                if (g.D != nullptr) {
+                    const chunk_t &a = d[2 * i], &b = d[2 * i + 1];
+                    v[0] += has ? __uint_as_float(a.x) : 0.f, v[1] += has ? __uint_as_float(a.y) : 0.f;
+                    v[2] += has ? __uint_as_float(a.z) : 0.f, v[3] += has ? __uint_as_float(a.w) : 0.f;
+                    v[4] += has ? __uint_as_float(b.x) : 0.f, v[5] += has ? __uint_as_float(b.y) : 0.f;
+                    v[6] += has ? __uint_as_float(b.z) : 0.f, v[7] += has ? __uint_as_float(b.w) : 0.f;
+                }
+                if (ok) store_columns(yrow, pc + i * 32, g.N, v);
+            }
         }
     }
 }
 
-template <int BM, int BN, int WM, int WN>
-hipError_t launch_t(const MxGemmArgs &a0, hipStream_t stream, const KernelTimer *timer) {
+template <int BM, int BN, int PARTS, bool SPLIT>
+hipError_t launch_s(const MxGemmArgs &a0, hipStream_t stream, const KernelTimer *timer) {
     MxGemmArgs a = a0;
     const int tiles_m = (a.T + BM - 1) / BM;
     int tiles_n = 0;
@@ -152,18 +469,60 @@ hipError_t launch_t(const MxGemmArgs &a0, hipStream_t stream, const KernelTimer 
     }
     const long total = (long)tiles_m * tiles_n;
     if (total <= 0) return hipSuccess;
-    return launch_kernel(mx_gemm_kernel<BM, BN, WM, WN>, dim3((unsigned)((total + 7) / 8 * 8)), dim3(WM * WN * 64), 0, stream, timer, a, tiles_m,
-                         tiles_n, 8);
+    return launch_kernel(mx_gemm_kernel<BM, BN, PARTS, SPLIT>, dim3((unsigned)((total + 7) / 8 * 8), SPLIT ? (unsigned)a.split_k : 1u), dim3(256),
+                         MxTile<BM, BN>::smem, stream, timer, a, tiles_m, tiles_n, 8);
+}
+template <int BM, int BN, int PARTS>
+hipError_t launch_p(const MxGemmArgs &a, hipStream_t stream, const KernelTimer *timer) {
+    return a.split_k > 1 ? launch_s<BM, BN, PARTS, true>(a, stream, timer) : launch_s<BM, BN, PARTS, false>(a, stream, timer);
+}
+template <int BM, int BN>
+hipError_t launch_t(const MxGemmArgs &a, hipStream_t stream, const KernelTimer *timer) {
+    return a.parts == 2 ? launch_p<BM, BN, 2>(a, stream, timer) : launch_p<BM, BN, 1>(a, stream, timer);
+}
+template <int BM, int BN>
+hipError_t init_t() {
+    const void *const kernels[4] = {reinterpret_cast<const void *>(mx_gemm_kernel<BM, BN, 1, false>), reinterpret_cast<const void *>(mx_gemm_kernel<BM, BN, 1, true>),
+                                    reinterpret_cast<const void *>(mx_gemm_kernel<BM, BN, 2, false>), reinterpret_cast<const void *>(mx_gemm_kernel<BM, BN, 2, true>)};
+    for (const void *k : kernels) {
+        const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)MxTile<BM, BN>::smem);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
-hipError_t init_mx_gemm_kernels() { return hipSuccess; }
+hipError_t init_mx_gemm_kernels() {
+    hipError_t e = init_t<256, 256>();
+    if (e == hipSuccess) e = init_t<256, 128>();
+    if (e == hipSuccess) e = init_t<128, 256>();
+    if (e == hipSuccess) e = init_t<128, 128>();
+    return e;
+}
 
 hipError_t launch_mx_gemm(const MxGemmArgs &a, int variant, hipStream_t stream, const KernelTimer *timer) {
-    if (!(a.T > 0 && a.K > 0 && a.K % kMxBlock == 0 && a.n_sets >= 1 && a.n_sets <= kMaxGemmSets && a.Xq && a.Xs)) return hipErrorInvalidValue;
-    (void)variant;
-    return launch_t<128, 128, 2, 2>(a, stream, timer);
+    if (!(a.T > 0 && a.K > 0 && a.K % kMxBlock == 0 && a.n_sets >= 1 && a.n_sets <= kMaxGemmSets && a.Xq && a.Xs && (a.parts == 1 || a.parts == 2)))
+        return hipErrorInvalidValue;
+    const int blocks = a.K / kMxBlock;
+    if (a.parts == 2 && (a.part_bytes < a.K || a.part_scales < blocks)) return hipErrorInvalidValue;
+    if (a.split_k > 1) {
+        if (a.n_sets != 1 || a.set[0].B || a.set[0].D || !a.P || a.ldp < a.set[0].N || (a.ldp & 7) || a.chunk_blocks <= 0 || a.chunk_blocks % 16 ||
+            (long)a.chunk_blocks * (a.split_k - 1) >= blocks || (long)a.chunk_blocks * a.split_k < blocks)
+            return hipErrorInvalidValue;
+    }
+    switch (variant) {
+        case kMxTile256x256:
+            return launch_t<256, 256>(a, stream, timer);
+        case kMxTile256x128:
+            return launch_t<256, 128>(a, stream, timer);
+        case kMxTile128x256:
+            return launch_t<128, 256>(a, stream, timer);
+        case kMxTile128x128:
+            return launch_t<128, 128>(a, stream, timer);
+        default:
+            return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace lora

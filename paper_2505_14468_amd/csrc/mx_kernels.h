@@ -67,6 +67,7 @@ hipError_t init_mx_decode_kernels();
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
 
 // More rows: tiles on 4-bit weights and 8-bit activations.
+enum MxTileVariant { kMxTile256x256 = 0, kMxTile256x128 = 1, kMxTile128x256 = 2, kMxTile128x128 = 3, kMxTileCount };
 struct MxGemmSet {
     const unsigned char *Wq;
     int64_t ldwq;
@@ -74,10 +75,14 @@ struct MxGemmSet {
     int64_t ldws;
     void *Y;
     int64_t ldy;
-    const float *D;  // adapter term in fp32, [T, ldd], rows with an adapter only (null: none)
+    const void *V;         // [T, r_max] bf16, original row order (null: no adapters)
+    const void *const *B;  // device table (null: no adapters, or all of the adapter term comes in D)
+    const float *D;        // adapter term in fp32, [T, ldd], rows with an adapter only (null: none)
     int64_t ldd;
+    int32_t long_rows;     // > 0: D holds the term of segments shorter than this, the kernel computes the others'
     int32_t N;
-    int32_t tile0;   // first column tile (set by the launcher)
+    int32_t tile0;         // first column tile (set by the launcher)
+    int32_t pad_;
 };
 struct MxGemmArgs {
     PlanView plan;
@@ -86,11 +91,33 @@ struct MxGemmArgs {
     const unsigned char *Xs;
     int64_t ldxs;
     int32_t T, K;
+    int32_t r_max;
+    int32_t parts;        // 1, or 2: X is the sum of two sets of values, part_bytes (a multiple of 512, zeros past K) and
+    int32_t part_bytes;   // part_scales apart in a row
+    int32_t part_scales;
+    // > 1: the contraction axis in stretches of chunk_blocks blocks (a multiple of 16); one projection, no adapter term here;
+    // partial sums to P[s][row][n], rows ldp floats long (launch_splitk_reduce sums them)
+    int32_t split_k;
+    int32_t chunk_blocks;
+    float *P;
+    int64_t ldp;
     int32_t n_sets;
     int32_t pad_;
     MxGemmSet set[kMaxGemmSets];
 };
 hipError_t init_mx_gemm_kernels();
 hipError_t launch_mx_gemm(const MxGemmArgs &a, int variant, hipStream_t stream, const KernelTimer *timer);
+
+// bf16 rows as the sum of two sets of 8-bit values (MxGemmArgs::parts == 2): codes [rows, 2 part_bytes], scales [rows, 2 part_scales].
+struct MxSplitArgs {
+    const void *X;
+    int64_t ldx;
+    unsigned char *codes;
+    unsigned char *scales;
+    int32_t rows, K;
+    int32_t part_bytes, part_scales;
+    int32_t strips;  // set by the launcher
+};
+hipError_t launch_mx_split(const MxSplitArgs &a, hipStream_t stream, const KernelTimer *timer);
 
 }  // namespace lora
