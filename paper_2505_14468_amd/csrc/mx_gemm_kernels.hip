@@ -23,9 +23,11 @@
 // The one barrier of a stage therefore stands where all of the stage has been read: its LDS takes the stage after next at once,
 // which then has a whole stage to arrive, and the next one has arrived.
 //
-// The extension runs behind the base product on bf16 16x16x32 MFMAs, segment by segment (the rows of a tile are in slot order, so
-// an adapter's are contiguous), with operands straight from memory: a few k-steps per tile, against K / 128 stages.  Rows of others
-// in a 16-row block meet zeros of V.
+// The extension is more stages of the same pipeline, of 32 ranks each, on bf16 16x16x32 MFMAs: the rows of a tile are in slot order, so
+// an adapter's are contiguous, and its V and B_a take the places of X and W in LDS (rows of B_a of 64 bytes are laid out as W's,
+// rows of V as the first halves of X's).  The first two are requested where the base product has nothing left to request.
+// Rows of other adapters and ranks past the adapter's own are loads out of the descriptor's range: zeros that cost no
+// traffic.  A tile's segments are found by one thread each and kept in a table.
 #include <type_traits>
 #include <utility>
 
@@ -99,7 +101,7 @@ struct MxTile {
     static constexpr int NT = 256, WTM = BM / 2, WTN = BN / 2, NBT = WTM / 16, NBN = WTN / 16, HT = NBT / 2, HN = NBN / 2;
     static constexpr int GX = BM / 32, GW = BN / 64;  // direct loads of a stage per wave
     static constexpr size_t x_bytes = (size_t)BM * 128, w_bytes = (size_t)BN * 64, s_bytes = (size_t)(BM + BN) * 16;
-    static constexpr size_t smem = 2 * (x_bytes + w_bytes + s_bytes) + (size_t)BM * 5;
+    static constexpr size_t smem = 2 * (x_bytes + w_bytes + s_bytes) + (size_t)BM * (16 + 4 + 1) + 16;
     static_assert(NBT % 2 == 0 && NBN % 2 == 0 && HT >= 1 && HN >= 1 && GX >= 1 && GW >= 1 && BM + BN <= 2 * NT && BM <= NT && BN <= NT, "tile shape");
 };
 
@@ -113,8 +115,10 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
     chunk_t *sX = reinterpret_cast<chunk_t *>(smem);                             // [2][BM * 8]
     chunk_t *sW = reinterpret_cast<chunk_t *>(smem + 2 * M::x_bytes);            // [2][BN * 4]
     chunk_t *sS = reinterpret_cast<chunk_t *>(smem + 2 * (M::x_bytes + M::w_bytes));  // [2][BM + BN], a superstage each
-    int *srow = reinterpret_cast<int *>(sS + 2 * (BM + BN));                     // tile row -> original row
-    unsigned char *use_d = reinterpret_cast<unsigned char *>(srow + BM);         // tile row takes its adapter term from D
+    chunk_t *sseg = sS + 2 * (BM + BN);                                          // the tile's segments whose term is computed here
+    int *srow = reinterpret_cast<int *>(sseg + BM);                              // tile row -> original row
+    int *scnt = srow + BM;                                                       // segments found per wave
+    unsigned char *use_d = reinterpret_cast<unsigned char *>(scnt + 4);          // tile row takes its adapter term from D
 
     // ---- workgroup -> tile: consecutive ids go round the 8 XCDs, each walks a contiguous, M-grouped range ----
     const int total = tiles_m * tiles_n;
@@ -219,17 +223,88 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         if (tid < BN) to[BM + tid] = transpose_scales(ws_new);
     };
     request_scales(0);
-    for_each<0, 2>([&](auto sc) __attribute__((always_inline)) {
-        stage_desc(sc.value);
-        for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, sc.value), wait_state(), load(jc); });
-    });
+    stage_desc(0);
+    for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, 0), wait_state(), load(jc); });
 
-    // ---- which rows take their adapter term from D (short segments', when the long ones' is computed here) ---------------
-    if (g.D != nullptr && tid < BM) {
-        const int s = p.plan.row_seg[min(m0 + tid, p.T - 1)];
-        const bool lng = g.long_rows > 0 && p.plan.seg_indptr[s + 1] - p.plan.seg_indptr[s] >= g.long_rows;
-        use_d[tid] = p.plan.seg_adapter[s] >= 0 && !lng;
+    // ---- the tile's segments: those whose term is computed here, and which rows take theirs from D ------------------------------
+    int n_seg = 0;
+    if (!SPLIT && (g.B != nullptr || g.D != nullptr)) {
+        const int m_last = min(m0 + BM, p.T) - 1;
+        const int s_first = p.plan.row_seg[m0], s_last = p.plan.row_seg[m_last];
+        if (g.D != nullptr && tid < BM) {
+            const int s = p.plan.row_seg[min(m0 + tid, m_last)];
+            const bool lng = g.long_rows > 0 && p.plan.seg_indptr[s + 1] - p.plan.seg_indptr[s] >= g.long_rows;
+            use_d[tid] = p.plan.seg_adapter[s] >= 0 && !lng;
+        }
+        if (g.B != nullptr) {  // (at most BM of them: each has a row here)
+            const int s = s_first + tid;
+            int lo = 0, hi = 0, r = 0;
+            const void *Ba = nullptr;
+            if (s <= s_last && tid < BM) {
+                const int ad = p.plan.seg_adapter[s];
+                lo = p.plan.seg_indptr[s], hi = p.plan.seg_indptr[s + 1], r = p.plan.seg_rank[s];
+                if (ad >= 0 && r > 0 && hi - lo >= g.long_rows) {
+                    Ba = g.B[ad];
+                    if (Ba == nullptr) atomicMin(&p.plan.scalars[kScEvicted], kErrNotResident);  // slot emptied after the plan
+                }
+            }
+            const unsigned long long found = __builtin_amdgcn_ballot_w64(Ba != nullptr);
+            if (lane == 0) scnt[wave] = __builtin_popcountll(found);
+            __syncthreads();
+            int at = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                at += w < wave ? scnt[w] : 0;
+                n_seg += scnt[w];
+            }
+            at += __builtin_popcountll(found & ((1ull << lane) - 1ull));
+            const uint64_t addr = reinterpret_cast<uint64_t>(Ba);
+            if (Ba != nullptr) sseg[at] = make_uint4((unsigned)addr, (unsigned)(addr >> 32), (unsigned)r, (unsigned)max(lo - m0, 0) | (unsigned)min(hi - m0, BM) << 16);
+            __syncthreads();
+            n_seg = __builtin_amdgcn_readfirstlane(n_seg);
+        }
     }
+    // The next extension stage: 32 ranks of a segment.  span: its tile rows, first | end << 16; 0: there is none.
+    int ext_seg = 0, ext_j = 0;
+    auto extension_desc = [&]() __attribute__((always_inline)) -> int {
+        if (ext_seg >= n_seg) {
+            Xd = make_buffer_desc(p.Xq, 0);
+            Wd = make_buffer_desc(p.Xq, 0);
+            return 0;
+        }
+        const chunk_t e = sseg[ext_seg];
+        const uint64_t addr = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)e.y) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)e.x);
+        const int r = __builtin_amdgcn_readfirstlane((int)e.z), span = __builtin_amdgcn_readfirstlane((int)e.w);
+        const int lo = span & 0xffff, hi = span >> 16, j0 = ext_j;
+        ext_j += 32;
+        if (ext_j >= r) ext_j = 0, ++ext_seg;
+        x_so = w_so = 0;
+        Xd = make_buffer_desc(g.V, (int)(unsigned)((int64_t)p.T * p.r_max * 2));
+        Wd = make_buffer_desc(reinterpret_cast<const E *>(addr) + (int64_t)n0 * r, min(BN, g.N - n0) * r * 2);
+#pragma unroll
+        for (int i = 0; i < GX; ++i) {
+            const int row = rx0 + i * 8 + (lane >> 3), j = j0 + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
+            ox[i] = row >= lo && row < hi && j < min(j0 + 32, r) ? (unsigned)srow[row] * (unsigned)(p.r_max * 2) + (unsigned)j * 2u : ~15u;
+        }
+#pragma unroll
+        for (int i = 0; i < GW; ++i) {
+            const int row = rw0 + i * 16 + 2 * (lane >> 3) + ((lane & 7) >> 2), j = j0 + ((lane & 3) ^ ((row >> 2) & 3)) * 8;
+            ow[i] = j < r ? (unsigned)(min(n0 + row, g.N - 1) - n0) * (unsigned)(r * 2) + (unsigned)j * 2u : ~15u;
+        }
+        return span;
+    };
+    int span0 = 0, span1 = 0;  // of the two extension stages requested last
+    auto next_desc = [&](int kt) __attribute__((always_inline)) {
+        if (SPLIT || kt < KT || n_seg == 0) {
+            stage_desc(kt);
+        } else {
+            span0 = span1;
+            span1 = extension_desc();
+        }
+    };
+    __syncthreads();  // (srow)
+    next_desc(1);
+    for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, 1), wait_state(), load(jc); });
 
     f32x4_t acc[NBN][NBT];
 #pragma unroll
@@ -299,7 +374,7 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
                     }
                 });
             });
-            stage_desc(kt + 2);
+            next_desc(kt + 2);
             quadrant(sc, 0, b, [&](auto) __attribute__((always_inline)) {});
             wait_vm_barrier<0>();  // the next stage is there; this one has been read by every wave
             if (is_tail(kt + 1)) zero_tail(buf ^ 1);
@@ -356,53 +431,32 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
             stage(kt + 3, sbuf, std::integral_constant<int, 3>{});
         }
     }
+    // ---- extension: stage e is in the LDS of stage KT + e -------------------------------------------------------------------
+    if (!SPLIT && n_seg > 0) {
+        int buf = KT & 1;
+        while (span0 != 0) {
+            const int lo = span0 & 0xffff, hi = span0 >> 16;
+            chunk_t w[NBN], x[NBT];
+#pragma unroll
+            for (int nb = 0; nb < NBN; ++nb) w[nb] = read_here(sW + buf * BN * 4 + w_at(wn0 + lr, lq) + nb * 64);
+#pragma unroll
+            for (int tb = 0; tb < NBT; ++tb) x[tb] = read_here(sX + buf * BM * 8 + x_at(wm0 + lr, lq) + tb * 128);
+#pragma unroll
+            for (int tb = 0; tb < NBT; ++tb) {
+                const int t0 = wm0 + tb * 16;
+                if (lo < t0 + 16 && hi > t0) {
+#pragma unroll
+                    for (int nb = 0; nb < NBN; ++nb) Elem<E>::mma_step(acc[nb][tb], w[nb], x[tb], 0);
+                }
+            }
+            wait_vm_barrier<0>();  // the next one is there; this one has been read by every wave
+            next_desc(KT);
+            if (span1 != 0) for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, buf), wait_state(), load(jc); });
+            buf ^= 1;
+        }
+    }
     settle();
     wait_vm<0>();  // (loads past the end: none may arrive in LDS that is another workgroup's by then)
-
-    // ---- extension --------------------------------------------------------------------------------------------------------
-    if (!SPLIT && g.B != nullptr) {
-        const E *V = static_cast<const E *>(g.V);
-        const int m_end = min(m0 + BM, p.T);
-        const int s_first = p.plan.row_seg[m0], s_last = p.plan.row_seg[m_end - 1];
-        for (int s = s_first; s <= s_last; ++s) {
-            const int lo = p.plan.seg_indptr[s], hi = p.plan.seg_indptr[s + 1], ad = p.plan.seg_adapter[s], r = p.plan.seg_rank[s];
-            if (ad < 0 || r <= 0 || hi - lo < g.long_rows) continue;
-            const E *Ba = static_cast<const E *>(g.B[ad]);
-            if (Ba == nullptr) {
-                if (tid == 0) atomicMin(&p.plan.scalars[kScEvicted], kErrNotResident);  // slot emptied after the plan
-                continue;
-            }
-            const int tlo = max(lo - m0, 0), thi = min(hi - m0, BM);  // tile rows of the segment
-            if (thi <= wm0 || tlo >= wm0 + M::WTM) continue;
-            for (int j0 = 0; j0 < r; j0 += 32) {
-                const int j = j0 + lq * 8;
-                const bool jok = j < r;
-                chunk_t wv[NBN], xv[NBT];
-#pragma unroll
-                for (int nb = 0; nb < NBN; ++nb) wv[nb] = load_chunk(Ba + (int64_t)min(n0 + wn0 + nb * 16 + lr, g.N - 1) * r + (jok ? j : 0));
-#pragma unroll
-                for (int tb = 0; tb < NBT; ++tb) xv[tb] = load_chunk(V + (int64_t)srow[wm0 + tb * 16 + lr] * p.r_max + (jok ? j : 0));
-#pragma unroll
-                for (int nb = 0; nb < NBN; ++nb) wv[nb] = keep_if(jok, wv[nb]);
-#pragma unroll
-                for (int tb = 0; tb < NBT; ++tb) {
-                    const int t = wm0 + tb * 16 + lr;
-                    xv[tb] = keep_if(jok && t >= tlo && t < thi, xv[tb]);
-                }
-                operand_settle(wv);
-                operand_settle(xv);
-#pragma unroll
-                for (int tb = 0; tb < NBT; ++tb) {
-                    const int t0 = wm0 + tb * 16;
-                    if (tlo < t0 + 16 && thi > t0) {
-#pragma unroll
-                        for (int nb = 0; nb < NBN; ++nb) Elem<E>::mma_step(acc[nb][tb], wv[nb], xv[tb], 0);
-                    }
-                }
-            }
-        }
-        settle();
-    }
 
     // ---- the single store of Y (or of a split's partial sums, in fp32) -----------------------------------------------------
     constexpr int NP = NBN / 2;
@@ -422,37 +476,53 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         }
     } else {
         E *Y = static_cast<E *>(g.Y);
-        chunk_t term[2][2 * NP];
-        auto fetch = [&](int tb, chunk_t(&d)[2 * NP]) __attribute__((always_inline)) {
-            const int t = wm0 + tb * 16 + lr;
-            const float *drow = g.D + (use_d[t] != 0 ? (int64_t)srow[t] * g.ldd : 0);
+        if (g.D == nullptr) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const float *src = drow + min(pc + i * 32, (int)g.ldd - 8);  // (columns past N: loaded, never stored)
-                d[2 * i] = load_chunk(src);
-                d[2 * i + 1] = load_chunk(src + 4);
-            }
-        };
-        if (g.D != nullptr) fetch(0, term[0]);
+            for (int tb = 0; tb < NBT; ++tb) {
+                const int t = wm0 + tb * 16 + lr;
+                E *yrow = Y + (int64_t)srow[t] * g.ldy;
 #pragma unroll
-        for (int tb = 0; tb < NBT; ++tb) {
-            const int t = wm0 + tb * 16 + lr;
-            const bool ok = m0 + t < p.T, has = g.D != nullptr && use_d[t] != 0;
-            E *yrow = Y + (int64_t)srow[t] * g.ldy;
-            if (g.D != nullptr && tb + 1 < NBT) fetch(tb + 1, term[(tb + 1) & 1]);  // (a block ahead of the stores)
-            const chunk_t(&d)[2 * NP] = term[tb & 1];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                float v[8];
-                pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
-                if (g.D != nullptr) {
-                    const chunk_t &a = d[2 * i], &b = d[2 * i + 1];
-                    v[0] += has ? __uint_as_float(a.x) : 0.f, v[1] += has ? __uint_as_float(a.y) : 0.f;
-                    v[2] += has ? __uint_as_float(a.z) : 0.f, v[3] += has ? __uint_as_float(a.w) : 0.f;
-                    v[4] += has ? __uint_as_float(b.x) : 0.f, v[5] += has ? __uint_as_float(b.y) : 0.f;
-                    v[6] += has ? __uint_as_float(b.z) : 0.f, v[7] += has ? __uint_as_float(b.w) : 0.f;
+                for (int i = 0; i < NP; ++i) {
+                    float v[8];
+                    pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
+                    if (m0 + t < p.T) store_columns(yrow, pc + i * 32, g.N, v);
                 }
-                if (ok) store_columns(yrow, pc + i * 32, g.N, v);
+            }
+        } else {
+            // (the term is read a row block ahead of the stores that it is added into)
+            chunk_t term[2][2 * NP];
+            auto fetch = [&](int tb, chunk_t(&d)[2 * NP]) __attribute__((always_inline)) {
+                const int t = wm0 + tb * 16 + lr;
+                const float *drow = g.D + (use_d[t] != 0 ? (int64_t)srow[t] * g.ldd : 0);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const float *src = drow + min(pc + i * 32, (int)g.ldd - 8);  // (columns past N: loaded, never stored)
+                    d[2 * i] = load_chunk(src);
+                    d[2 * i + 1] = load_chunk(src + 4);
+                }
+            };
+            auto add4 = [](float *v, bool has, const chunk_t &d) __attribute__((always_inline)) {
+                v[0] += has ? __uint_as_float(d.x) : 0.f;
+                v[1] += has ? __uint_as_float(d.y) : 0.f;
+                v[2] += has ? __uint_as_float(d.z) : 0.f;
+                v[3] += has ? __uint_as_float(d.w) : 0.f;
+            };
+            fetch(0, term[0]);
+#pragma unroll
+            for (int tb = 0; tb < NBT; ++tb) {
+                const int t = wm0 + tb * 16 + lr;
+                const bool ok = m0 + t < p.T, has = use_d[t] != 0;
+                E *yrow = Y + (int64_t)srow[t] * g.ldy;
+                if (tb + 1 < NBT) fetch(tb + 1, term[(tb + 1) & 1]);
+                const chunk_t(&d)[2 * NP] = term[tb & 1];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    float v[8];
+                    pair_columns(acc[2 * i][tb], acc[2 * i + 1][tb], v);
+                    add4(v, has, d[2 * i]);
+                    add4(v + 4, has, d[2 * i + 1]);
+                    if (ok) store_columns(yrow, pc + i * 32, g.N, v);
+                }
             }
         }
     }

@@ -1,0 +1,47 @@
+"""Wait states around the matrix instructions of the tiles on 4-bit weights, read back from the built library (they are assembly that the
+compiler does not know as such; see test_mfma_code_cpu, whose reader and rules these are)."""
+import re
+import shutil
+import subprocess
+
+import pytest
+
+import test_mfma_code_cpu as code_check
+from paper_2505_14468_amd.build import LIB_PATH
+
+pytestmark = pytest.mark.skipif(not shutil.which(code_check.LLVM + "llvm-objdump"), reason="no disassembler")
+
+SCALED_TO_ACCESS = 12  # a block-scaled 16x16x128 MFMA, then anything else that touches its accumulator
+
+
+def _kernels(obj):
+    text = subprocess.run([code_check.LLVM + "llvm-objdump", "-d", "--mcpu=gfx950", str(obj)], check=True, stdout=subprocess.PIPE, text=True).stdout
+    for name, body in re.findall(r"^[0-9a-f]+ <(\S*mx_gemm_kernel\S*)>:\n(.*?)(?=^[0-9a-f]+ <|\Z)", text, re.S | re.M):
+        code, base = [], None
+        for line in body.splitlines():
+            m = re.match(r"\s+(\S.*?)\s*// ([0-9A-F]+):", line)
+            if not m or m[1].startswith("."):
+                continue
+            addr = int(m[2], 16)
+            base = addr if base is None else base
+            t = re.search(r"<\S+\+0x([0-9a-f]+)>", line) if "branch" in m[1] else None
+            code.append(code_check.Instr(addr, m[1], base + int(t[1], 16) if t else (base if "branch" in m[1] else None)))
+        yield name, code
+
+
+def test_wait_states_of_every_tile(tmp_path):
+    found = {}
+    for k, data in enumerate(code_check.code_objects(LIB_PATH, tmp_path)):
+        if b"mx_gemm_kernel" in data:
+            obj = tmp_path / f"object_{k}"
+            obj.write_bytes(data)
+            found.update(_kernels(obj))
+    assert len(found) == 16  # four tiles, one or two parts, whole or split
+    for name, code in found.items():
+        scaled = [x for x in code if x.op.startswith("v_mfma_scale")]
+        assert len(scaled) >= 64 and sum(x.lds_load for x in code) >= 6, name
+        assert not code_check.faults(code), (name, code_check.faults(code)[:3])
+        prev = code_check.before(code)
+        since = code_check.states_since(code, prev, lambda x: x.op.startswith("v_mfma_scale"))
+        close = [(x.text, since[i]) for i, x in enumerate(code) if not x.mfma and any(k == "a" for k, _ in x.regs) and since[i] < SCALED_TO_ACCESS]
+        assert not close, (name, close[:3])
