@@ -11,21 +11,22 @@
 // Activations of PARTS == 2 come as the sum of two sets of 8-bit values (a bf16 row taken apart, mx_split_kernel): the
 // contraction axis is walked twice, once for each, against the same W.
 //
-// Tile: BM rows x BN columns, stages of 128 values of the contraction axis, two of them in LDS, loaded there directly.  4
+// Tile: BM rows x BN columns, stages of 128 values of the contraction axis, D of them in LDS, loaded there directly.  4
 // waves, one per SIMD, each a quarter of the tile.  What a stage costs a wave besides its MFMAs (256 x 256: 64 of them, 32
 // cycles each) is 24 operand reads, 12 loads and a few scalar instructions, dealt out one behind an MFMA; the scales cost
-// nothing there: of four stages together they are read once, in the order that the instruction wants them (below).
+// next to nothing: they are loaded, put into the order that the instruction wants and read once for four stages together.
 //
 // The wave's tile is cut into halves along both sides, W0 W1 and X0 X1; a stage multiplies its four quadrants in the order
 //     (W0, Xa) (W0, Xb) | barrier | (W1, Xb) (W1, Xa)         a = 0, b = 1 in even stages, the reverse in odd ones
 // so that every half of the operands is free a quadrant before the next stage's takes its registers: Xb and W1 are read from LDS
 // during the first quadrant, W0 of the next stage during the third, its first X half (this one's Xb) during the fourth.
-// The one barrier of a stage therefore stands where all of the stage has been read: its LDS takes the stage after next at once,
-// which then has a whole stage to arrive, and the next one has arrived.
+// The one barrier of a stage therefore stands where all of the stage has been read: its LDS takes stage kt + D at once, which then has
+// D - 1 stages to arrive.  256 x 256: D = 2 (a stage is 2048 cycles of MFMAs); 128 x 256 and 128 x 128, whose stages are a half and a
+// quarter of that, D = 4.
 //
 // The extension is more stages of the same pipeline, of 32 ranks each, on bf16 16x16x32 MFMAs: the rows of a tile are in slot order, so
 // an adapter's are contiguous, and its V and B_a take the places of X and W in LDS (rows of B_a of 64 bytes are laid out as W's,
-// rows of V as the first halves of X's).  The first two are requested where the base product has nothing left to request.
+// rows of V as the first halves of X's).  The first are requested where the base product has nothing left to request.
 // Rows of other adapters and ranks past the adapter's own are loads out of the descriptor's range: zeros that cost no
 // traffic.  A tile's segments are found by one thread each and kept in a table.
 #include <type_traits>
@@ -96,12 +97,25 @@ __device__ __forceinline__ chunk_t load_scales(const unsigned char *row, int s, 
     return make_uint4(d[0], d[1], d[2], d[3]);
 }
 
+// A direct load whose descriptor or offset a vector instruction may just have written (a lane read into a scalar register, which is also
+// how the compiler brings back scalars it had no room for): 5 wait states, which it keeps in front of its own loads only.  The
+// loads of a stage do without: they are a quadrant away from the scalars they use, which is checked in the built code.
+__device__ __forceinline__ void load_to_lds_settled(const BufferDesc &d, unsigned lane_off, int scalar_off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(lane_off), "s"(d.r), "s"(scalar_off));
+#else
+    (void)d, (void)lane_off, (void)scalar_off;
+#endif
+}
+
 template <int BM, int BN>
 struct MxTile {
     static constexpr int NT = 256, WTM = BM / 2, WTN = BN / 2, NBT = WTM / 16, NBN = WTN / 16, HT = NBT / 2, HN = NBN / 2;
     static constexpr int GX = BM / 32, GW = BN / 64;  // direct loads of a stage per wave
+    static constexpr int D = BM * BN >= 65536 ? 2 : 4;  // stages in LDS
     static constexpr size_t x_bytes = (size_t)BM * 128, w_bytes = (size_t)BN * 64, s_bytes = (size_t)(BM + BN) * 16;
-    static constexpr size_t smem = 2 * (x_bytes + w_bytes + s_bytes) + (size_t)BM * (16 + 4 + 1) + 16;
+    static constexpr size_t smem = D * (x_bytes + w_bytes) + 3 * s_bytes + (size_t)BM * (16 + 4 + 1) + 16;
+    static_assert(smem <= 160 * 1024, "LDS of a CU");
     static_assert(NBT % 2 == 0 && NBN % 2 == 0 && HT >= 1 && HN >= 1 && GX >= 1 && GW >= 1 && BM + BN <= 2 * NT && BM <= NT && BN <= NT, "tile shape");
 };
 
@@ -109,12 +123,13 @@ template <int BM, int BN, int PARTS, bool SPLIT>
 __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m, int tiles_n, int group_m) {
     typedef MxTile<BM, BN> M;
     typedef __bf16 E;
-    constexpr int NBT = M::NBT, NBN = M::NBN, HT = M::HT, HN = M::HN, GX = M::GX, GW = M::GW;
+    constexpr int NBT = M::NBT, NBN = M::NBN, HT = M::HT, HN = M::HN, GX = M::GX, GW = M::GW, D = M::D;
 
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    chunk_t *sX = reinterpret_cast<chunk_t *>(smem);                             // [2][BM * 8]
-    chunk_t *sW = reinterpret_cast<chunk_t *>(smem + 2 * M::x_bytes);            // [2][BN * 4]
-    chunk_t *sS = reinterpret_cast<chunk_t *>(smem + 2 * (M::x_bytes + M::w_bytes));  // [2][BM + BN], a superstage each
+    chunk_t *sX = reinterpret_cast<chunk_t *>(smem);                             // [D][BM * 8]
+    chunk_t *sW = reinterpret_cast<chunk_t *>(smem + D * M::x_bytes);            // [D][BN * 4]
+    chunk_t *sraw = sW + D * BN * 4;                                             // [BM + BN]: the next superstage's scales as they lie in memory
+    chunk_t *sS = sraw + (BM + BN);                                              // [2][BM + BN]: two superstages' in order
     chunk_t *sseg = sS + 2 * (BM + BN);                                          // the tile's segments whose term is computed here
     int *srow = reinterpret_cast<int *>(sseg + BM);                              // tile row -> original row
     int *scnt = srow + BM;                                                       // segments found per wave
@@ -207,24 +222,48 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         else
             load_to_lds(Wd, ow[j - GX], w_so);
     };
-    // ---- scales: thread t takes row t of W's tile and row t of X's; a superstage of both parts has the same of W -----------
-    const unsigned char *xs_row = p.Xs + (int64_t)my_row * p.ldxs + b0, *ws_row = g.Ws + (int64_t)min(n0 + tid % BN, g.N - 1) * g.ldws + b0;
-    const int SP = (KP + 3) >> 2;  // superstages of a part
-    chunk_t xs_new, ws_new;
-    auto request_scales = [&](int s) __attribute__((always_inline)) {
-        int k = s, part = 0;
-        if constexpr (PARTS == 2) part = s >= SP ? 1 : 0, k = s - (part ? SP : 0);
-        xs_new = load_scales(xs_row + part * p.part_scales, k, nloc);
-        ws_new = load_scales(ws_row, k, nloc);
+    auto load_settled = [&](auto jc) __attribute__((always_inline)) {
+        constexpr int j = jc.value;
+        if constexpr (j < GX)
+            load_to_lds_settled(Xd, ox[j], x_so);
+        else
+            load_to_lds_settled(Wd, ow[j - GX], w_so);
     };
-    auto store_scales = [&](int s) __attribute__((always_inline)) {
+    // ---- scales, a superstage (four stages) at a time: thread t takes rows t of X's and of W's tile (those of a smaller tile are loaded
+    // twice).  Whole superstages are loaded straight into LDS, in front of a stage's loads and like them unknown to the
+    // compiler, which would wait for everything in flight with them; a last, partial one through registers, masked. ------------
+    const int SP = (KP + 3) >> 2;  // superstages of a part
+    const int xs_range = (int)(unsigned)((int64_t)p.T * p.ldxs - b0), ws_range = (int)(unsigned)((int64_t)min(BN, g.N - n0) * g.ldws - b0);
+    const BufferDesc Xsd = make_buffer_desc(p.Xs + b0, xs_range), Wsd = make_buffer_desc(g.Ws + (int64_t)n0 * g.ldws + b0, ws_range);
+    const unsigned oxs = (unsigned)((int64_t)my_row * p.ldxs), ows = (unsigned)((int64_t)(min(n0 + tid % BN, g.N - 1) - n0) * g.ldws);
+    const unsigned dxs = lds_address(sraw) + (unsigned)(wave % (BM / 64)) * 1024u, dws = lds_address(sraw) + (unsigned)(BM * 16 + wave % (BN / 64) * 1024);
+    chunk_t xs_new = zero_chunk(), ws_new = zero_chunk();
+    auto request_scales = [&](int s) __attribute__((always_inline)) {
+        const int part = PARTS == 2 && s >= SP ? 1 : 0, k = s - (part ? SP : 0);
+        const int xo = __builtin_amdgcn_readfirstlane(part * p.part_scales + k * 16), wo = __builtin_amdgcn_readfirstlane(k * 16);
+        if (k * 16 + 16 <= nloc) {
+            set_lds_base<0>(dxs), load_to_lds_settled(Xsd, oxs, xo);
+            set_lds_base<0>(dws), load_to_lds_settled(Wsd, ows, wo);
+        } else {
+            xs_new = load_scales(p.Xs + b0 + (int64_t)my_row * p.ldxs + part * p.part_scales, k, nloc);
+            ws_new = load_scales(g.Ws + b0 + (int64_t)min(n0 + tid % BN, g.N - 1) * g.ldws, k, nloc);
+        }
+    };
+    auto order_scales = [&](int s) __attribute__((always_inline)) {
         chunk_t *to = sS + (s & 1) * (BM + BN);
-        if (tid < BM) to[tid] = transpose_scales(xs_new);
-        if (tid < BN) to[BM + tid] = transpose_scales(ws_new);
+        const int k = PARTS == 2 && s >= SP ? s - SP : s;
+        if (k * 16 + 16 <= nloc) {
+#pragma unroll
+            for (int i = 0; i < (BM + BN + 255) / 256; ++i)
+                if ((BM + BN) % 256 == 0 || tid + i * 256 < BM + BN) to[tid + i * 256] = transpose_scales(sraw[tid + i * 256]);
+        } else {
+            if (tid < BM) to[tid] = transpose_scales(xs_new);
+            if (tid < BN) to[BM + tid] = transpose_scales(ws_new);
+        }
     };
     request_scales(0);
     stage_desc(0);
-    for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, 0), wait_state(), load(jc); });
+    for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, 0), load_settled(jc); });
 
     // ---- the tile's segments: those whose term is computed here, and which rows take theirs from D ------------------------------
     int n_seg = 0;
@@ -293,18 +332,21 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         }
         return span;
     };
-    int span0 = 0, span1 = 0;  // of the two extension stages requested last
+    int span[D] = {};  // of the extension stages requested last, the oldest first
     auto next_desc = [&](int kt) __attribute__((always_inline)) {
         if (SPLIT || kt < KT || n_seg == 0) {
             stage_desc(kt);
         } else {
-            span0 = span1;
-            span1 = extension_desc();
+#pragma unroll
+            for (int i = 0; i + 1 < D; ++i) span[i] = span[i + 1];
+            span[D - 1] = extension_desc();
         }
     };
     __syncthreads();  // (srow)
-    next_desc(1);
-    for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, 1), wait_state(), load(jc); });
+    for_each<1, D>([&](auto sc) __attribute__((always_inline)) {
+        next_desc(sc.value);
+        for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, sc.value), load_settled(jc); });
+    });
 
     f32x4_t acc[NBN][NBT];
 #pragma unroll
@@ -359,7 +401,7 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
             });
         };
         auto stage = [&](int kt, int sbuf, auto sc) __attribute__((always_inline)) {
-            constexpr int s = sc.value, buf = s & 1, a = s & 1, b = a ^ 1;
+            constexpr int s = sc.value, buf = s % D, next = (s + 1) % D, a = s & 1, b = a ^ 1;
             // first quadrant: the other halves of this stage, X's first
             quadrant(sc, 0, a, [&](auto ic) __attribute__((always_inline)) {
                 constexpr int i = ic.value, R = 2 * HT + HN;
@@ -374,17 +416,17 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
                     }
                 });
             });
-            next_desc(kt + 2);
+            next_desc(kt + D);
             quadrant(sc, 0, b, [&](auto) __attribute__((always_inline)) {});
-            wait_vm_barrier<0>();  // the next stage is there; this one has been read by every wave
-            if (is_tail(kt + 1)) zero_tail(buf ^ 1);
+            wait_vm_barrier<(D - 2) * GL>();  // the next stage is there (the D - 2 behind it may not be); this one has been read by every wave
+            if (is_tail(kt + 1)) zero_tail(next);
             if constexpr (s == 0) {
                 if (kt + 4 < KT) request_scales((kt >> 2) + 1);
             }
-            if constexpr (s == 1) {
-                if (kt + 3 < KT) store_scales((kt >> 2) + 1);  // (read from stage 3 on; its buffer was last read in the stage before this)
+            if constexpr (s == 2) {  // (there since this barrier at the latest; read from stage 3's on; that buffer was last read in stage 0)
+                if (kt + 2 < KT) order_scales((kt >> 2) + 1);
             }
-            // third and fourth quadrant: W0, then Xb of the next stage; the stage after next is requested
+            // third and fourth quadrant: W0, then Xb of the next stage; stage kt + D is requested
             auto loads = [&](auto ic) __attribute__((always_inline)) {  // (i: of 2 Q MFMAs; where a load goes is set one MFMA ahead)
                 constexpr int i = ic.value;
                 for_each<0, GL>([&](auto jc) __attribute__((always_inline)) {
@@ -397,7 +439,7 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
             quadrant(sc, 1, b, [&](auto ic) __attribute__((always_inline)) {
                 constexpr int i = ic.value;
                 for_each<i * HN / Q, (i + 1) * HN / Q>([&](auto jc) __attribute__((always_inline)) {
-                    read_w(0, jc.value, buf ^ 1);
+                    read_w(0, jc.value, next);
                     if constexpr (s == 3) read_ws(0, jc.value, sbuf ^ 1);
                 });
                 loads(ic);
@@ -405,15 +447,15 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
             quadrant(sc, 1, a, [&](auto ic) __attribute__((always_inline)) {
                 constexpr int i = ic.value;
                 for_each<i * 2 * HT / Q, (i + 1) * 2 * HT / Q>([&](auto jc) __attribute__((always_inline)) {
-                    read_x(b, jc.value / 2, jc.value % 2, buf ^ 1);
+                    read_x(b, jc.value / 2, jc.value % 2, next);
                     if constexpr (s == 3 && jc.value % 2 == 0) read_xs(b, jc.value / 2, sbuf ^ 1);
                 });
                 loads(std::integral_constant<int, i + Q>{});
             });
         };
-        store_scales(0);
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what is loaded in front of the loop has arrived, and the compiler knows
-        wait_vm_barrier<0>();
+        wait_vm_barrier<(D - 1) * GL>();  // the scales and the first stage are there
+        order_scales(0);
+        __syncthreads();
         if (is_tail(0)) zero_tail(0);
 #pragma unroll
         for (int i = 0; i < HN; ++i) read_w(0, i, 0), read_ws(0, i, 0);
@@ -421,21 +463,16 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         for (int i = 0; i < HT; ++i) read_x(0, i, 0, 0), read_x(0, i, 1, 0), read_xs(0, i, 0);
 #pragma clang loop unroll(disable)
         for (int kt = 0; kt < KT; kt += 4) {
-            const int sbuf = (kt >> 2) & 1;
-            stage(kt, sbuf, std::integral_constant<int, 0>{});
-            if (kt + 1 >= KT) break;
-            stage(kt + 1, sbuf, std::integral_constant<int, 1>{});
-            if (kt + 2 >= KT) break;
-            stage(kt + 2, sbuf, std::integral_constant<int, 2>{});
-            if (kt + 3 >= KT) break;
-            stage(kt + 3, sbuf, std::integral_constant<int, 3>{});
+            for_each<0, 4>([&](auto sc) __attribute__((always_inline)) {
+                if (kt + sc.value < KT) stage(kt + sc.value, (kt >> 2) & 1, sc);
+            });
         }
     }
     // ---- extension: stage e is in the LDS of stage KT + e -------------------------------------------------------------------
     if (!SPLIT && n_seg > 0) {
-        int buf = KT & 1;
-        while (span0 != 0) {
-            const int lo = span0 & 0xffff, hi = span0 >> 16;
+        int buf = KT % D;
+        while (span[0] != 0) {
+            const int lo = span[0] & 0xffff, hi = span[0] >> 16;
             chunk_t w[NBN], x[NBT];
 #pragma unroll
             for (int nb = 0; nb < NBN; ++nb) w[nb] = read_here(sW + buf * BN * 4 + w_at(wn0 + lr, lq) + nb * 64);
@@ -449,10 +486,10 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
                     for (int nb = 0; nb < NBN; ++nb) Elem<E>::mma_step(acc[nb][tb], w[nb], x[tb], 0);
                 }
             }
-            wait_vm_barrier<0>();  // the next one is there; this one has been read by every wave
-            next_desc(KT);
-            if (span1 != 0) for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, buf), wait_state(), load(jc); });
-            buf ^= 1;
+            wait_vm_barrier<(D - 2) * (GX + GW)>();  // the next one is there; this one has been read by every wave
+            next_desc(KT);  // (no bytes behind the last one: the counts stay what they are)
+            for_each<0, GX + GW>([&](auto jc) __attribute__((always_inline)) { load_base(jc, buf), load_settled(jc); });
+            buf = buf + 1 == D ? 0 : buf + 1;
         }
     }
     settle();
@@ -565,7 +602,6 @@ hipError_t init_t() {
 
 hipError_t init_mx_gemm_kernels() {
     hipError_t e = init_t<256, 256>();
-    if (e == hipSuccess) e = init_t<256, 128>();
     if (e == hipSuccess) e = init_t<128, 256>();
     if (e == hipSuccess) e = init_t<128, 128>();
     return e;
@@ -584,8 +620,6 @@ hipError_t launch_mx_gemm(const MxGemmArgs &a, int variant, hipStream_t stream, 
     switch (variant) {
         case kMxTile256x256:
             return launch_t<256, 256>(a, stream, timer);
-        case kMxTile256x128:
-            return launch_t<256, 128>(a, stream, timer);
         case kMxTile128x256:
             return launch_t<128, 256>(a, stream, timer);
         case kMxTile128x128:

@@ -67,7 +67,7 @@ hipError_t init_mx_decode_kernels();
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
 
 // More rows: tiles on 4-bit weights and 8-bit activations.
-enum MxTileVariant { kMxTile256x256 = 0, kMxTile256x128 = 1, kMxTile128x256 = 2, kMxTile128x128 = 3, kMxTileCount };
+enum MxTileVariant { kMxTile256x256 = 0, kMxTile128x256 = 1, kMxTile128x128 = 2, kMxTileCount };
 struct MxGemmSet {
     const unsigned char *Wq;
     int64_t ldwq;

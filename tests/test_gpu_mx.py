@@ -312,6 +312,45 @@ def test_layer_normal_values(T, K, N, ranks, x8):
     _check_close(Layer(T, K, [N], ranks, x8))
 
 
+@pytest.mark.parametrize("tile", [0, 1, 2])
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T,K,N", [(129, 32, 40), (257, 128, 300), (300, 544, 513), (200, 1600, 260), (700, 2080, 270), (513, 4128, 257)])
+def test_every_tile_and_split(T, K, N, x8, tile):
+    """Each tile, whole and split along K into as many stretches as there are superstages of 512 values, up to 8."""
+    c, rt, mx = _tools()
+    layer = Layer(T, K, [N], (8, 40, 128), x8, whole=True)
+    want = _bf16(layer.ref[0][0])[1]
+    assert layer.ref[0][1].max() < 2 ** 24
+    ws = torch.empty(mx.lora_mx_linear_workspace_bytes(T, K, N, 128, int(x8)) + 8 * T * (N + 7) * 4 + 4096, dtype=torch.uint8, device=c.device)
+    try:
+        c.set_option("mx_tile", tile)
+        for splits in (1, 2, 3, 5, 8):
+            for expand in (-1, 0, 1):  # the adapter term: by the batch's own rule, all in the tile, short segments' from memory
+                c.set_option("mx_split_k", splits)
+                c.set_option("expand_split", expand)
+                Y = mx.linear(c, layer.plan, layer.Xt, *layer.proj[0], Xq=layer.Xq, ws=ws)
+                assert torch.equal(Y.cpu(), want), (splits, expand, np.argwhere(_f64(Y) != want.double().numpy())[:4])
+    finally:
+        for name in ("mx_tile", "mx_split_k", "expand_split"):
+            c.set_option(name, -1)
+
+
+@pytest.mark.parametrize("tile", [0, 1, 2])
+def test_many_segments_in_a_tile(tile):
+    """A row to a segment, and segments of every length, with the whole adapter term in the tile."""
+    c, rt, mx = _tools()
+    n = 150
+    layer = Layer(400, 544, [140], tuple([8, 16, 24, 72][i % 4] for i in range(n)), True, whole=True)
+    try:
+        c.set_option("mx_tile", tile)
+        for expand in (0, 1):
+            c.set_option("expand_split", expand)
+            _check_whole(layer)
+    finally:
+        c.set_option("mx_tile", -1)
+        c.set_option("expand_split", -1)
+
+
 @pytest.mark.parametrize("x8", [False, True])
 @pytest.mark.parametrize("T", [3, 80, 128, 170])
 def test_nan_scale_stays_in_its_column(T, x8):
