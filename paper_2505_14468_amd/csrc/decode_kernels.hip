@@ -270,7 +270,7 @@ __global__ __launch_bounds__(TBLK * 64) void decode_reduce_kernel(DecodeArgs p0)
     if (a < 0 || r <= 0) Bp = nullptr;
     const float4 *P4 = reinterpret_cast<const float4 *>(p.P);
     const int64_t sstride = (int64_t)TBLK * 64;
-    const float4 *pb = P4 + ((int64_t)(p.nbe_cap + cb) * p.ks * TBLK + tb) * 64 + li * 4 + lg;
+    const float4 *pb = P4 + (((int64_t)p.nbe_cap * p.ks_ext + (int64_t)cb * p.ks) * TBLK + tb) * 64 + li * 4 + lg;
     float4 pq[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) pq[s] = pb[min(s, p.ks - 1) * sstride];
@@ -297,18 +297,18 @@ __global__ __launch_bounds__(TBLK * 64) void decode_reduce_kernel(DecodeArgs p0)
 #pragma unroll
             for (int i = 0; i < RQ; ++i) {
                 const int e = e0 + min(j0 + 4 * (lg + 4 * i), r - 4);
-                pv[i] = P4 + ((int64_t)(e >> 4) * p.ks * TBLK + tb) * 64 + li * 4 + ((e & 15) >> 2);
+                pv[i] = P4 + ((int64_t)(e >> 4) * p.ks_ext * TBLK + tb) * 64 + li * 4 + ((e & 15) >> 2);
                 q[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            for (int s0 = 0; s0 < p.ks; s0 += 8) {
+            for (int s0 = 0; s0 < p.ks_ext; s0 += 8) {
                 float4 g[8][RQ];
 #pragma unroll
                 for (int s = 0; s < 8; ++s)
 #pragma unroll
-                    for (int i = 0; i < RQ; ++i) g[s][i] = pv[i][min(s0 + s, p.ks - 1) * sstride];
+                    for (int i = 0; i < RQ; ++i) g[s][i] = pv[i][min(s0 + s, p.ks_ext - 1) * sstride];
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
-                    const float m = s0 + s < p.ks ? 1.f : 0.f;
+                    const float m = s0 + s < p.ks_ext ? 1.f : 0.f;
 #pragma unroll
                     for (int i = 0; i < RQ; ++i) {
                         q[i].x += m * g[s][i].x;
@@ -425,15 +425,15 @@ __device__ __forceinline__ void finish_unit(const DecodeArgs &p, const __bf16 *B
         for (int q = tid; q < nrows * quads; q += kFinWaves * 64) {
             const int i = q / quads, j = (q - i * quads) * 4;
             const int t = p.plan.perm[slot0 + i], e = e0 + j;
-            const float4 *src = P4 + ((int64_t)(e >> 4) * p.ks * TBLK + (t >> 4)) * 64 + (t & 15) * 4 + ((e & 15) >> 2);
+            const float4 *src = P4 + ((int64_t)(e >> 4) * p.ks_ext * TBLK + (t >> 4)) * 64 + (t & 15) * 4 + ((e & 15) >> 2);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int s0 = 0; s0 < p.ks; s0 += 8) {
+            for (int s0 = 0; s0 < p.ks_ext; s0 += 8) {
                 float4 g[8];
 #pragma unroll
-                for (int s = 0; s < 8; ++s) g[s] = src[min(s0 + s, p.ks - 1) * sstride];
+                for (int s = 0; s < 8; ++s) g[s] = src[min(s0 + s, p.ks_ext - 1) * sstride];
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
-                    const float m = s0 + s < p.ks ? 1.f : 0.f;
+                    const float m = s0 + s < p.ks_ext ? 1.f : 0.f;
                     v.x += m * g[s].x;
                     v.y += m * g[s].y;
                     v.z += m * g[s].z;
@@ -473,7 +473,7 @@ __device__ __forceinline__ void finish_unit(const DecodeArgs &p, const __bf16 *B
         const int i = q / (kFinCols / 4), ln = (q - i * (kFinCols / 4)) * 4, n = n00 + ln;
         if (n >= p.N) continue;
         const int t = p.plan.perm[slot0 + i];
-        const float4 *src = P4 + ((int64_t)(p.nbe_cap + (n >> 4)) * p.ks * TBLK + (t >> 4)) * 64 + (t & 15) * 4 + ((n & 15) >> 2);
+        const float4 *src = P4 + (((int64_t)p.nbe_cap * p.ks_ext + (int64_t)(n >> 4) * p.ks) * TBLK + (t >> 4)) * 64 + (t & 15) * 4 + ((n & 15) >> 2);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int s0 = 0; s0 < p.ks; s0 += 8) {
             float4 g[8];
@@ -650,7 +650,7 @@ hipError_t launch_reduce_t(const DecodeArgs &a, hipStream_t stream, const Kernel
 
 bool decode_args_ok(const DecodeArgs &a, int tblk) {
     if (!(a.T > (tblk - 1) * 16 && a.T <= tblk * 16 && a.K > 0 && (a.K & 7) == 0 && a.nbe >= 0 && a.nbe <= a.nbe_cap && a.X != nullptr &&
-          a.slice_chunks > 0 && a.ks == (a.K / 8 + a.slice_chunks - 1) / a.slice_chunks && a.n_sets >= 0 && a.n_sets <= kMaxGemmSets))
+          a.slice_chunks > 0 && a.ks_ext > 0 && a.ks == (a.K / 8 + a.slice_chunks - 1) / a.slice_chunks && a.n_sets >= 0 && a.n_sets <= kMaxGemmSets))
         return false;
     if (a.n_sets == 0) return a.N > 0 && a.nbw == (a.N + 15) / 16 && a.P != nullptr && a.W != nullptr && a.Y != nullptr;
     for (int i = 0; i < a.n_sets; ++i) {
@@ -676,7 +676,7 @@ hipError_t init_decode_kernels() {
 
 // tblk: 16-row blocks of the batch (1 .. 8).
 hipError_t launch_decode_stream(const DecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer) {
-    if (!decode_args_ok(a, tblk) || a.slice_chunks != kDsSliceChunks) return hipErrorInvalidValue;
+    if (!decode_args_ok(a, tblk) || a.slice_chunks != kDsSliceChunks || a.ks_ext != a.ks) return hipErrorInvalidValue;
     switch (tblk) {
         case 1:
             return launch_stream_t<1, kDecodeMaxWaves>(a, stream, timer);

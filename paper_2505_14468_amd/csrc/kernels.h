@@ -274,15 +274,16 @@ struct DecodeArgs {
     const float *scale;
     void *Y;
     int64_t ldy;
-    float *P;              // workspace: fp32 partial tiles, [nbe_cap + nbw][ks][tblk][16 tokens][16 weight rows]
+    float *P;              // workspace: fp32 partial tiles, [nbe_cap][ks_ext], then [nbw][ks], each [tblk][16 tokens][16 weight rows]
     int32_t T, K, N;
     int32_t r_max;         // the plan's largest rank
     int32_t n_adapters;    // entries of the A / B / scale tables
     int32_t nbw;           // blocks of 16 rows of W0: ceil(N / 16)
     int32_t nbe_cap;       // most blocks of 16 extension rows (rows of the used A_a) of any batch of the plan's sizes; they come first in P
     int32_t nbe;           // those the grid has room for (at most nbe_cap)
-    int32_t ks;            // slices along K
-    int32_t slice_chunks = 64; // their length in 16-byte chunks (decode_stream_kernel: 64, which is 512 values)
+    int32_t ks;            // slices along K of the base product's partial tiles
+    int32_t ks_ext;        // ... of the extension's (decode_stream_kernel: the same)
+    int32_t slice_chunks = 64; // length of the former in 16-byte chunks (decode_stream_kernel: 64, which is 512 values)
     int32_t waves;         // waves (= 16-row blocks) per workgroup of the streaming kernel
     long long *trace = nullptr;  // phase stamps (trace builds only)
     int32_t n_sets = 0;    // > 0: the projections of the launch (W .. P, N, nbw, n_adapters above are then unused)

@@ -746,7 +746,7 @@ DecodeArgs decode_args(const lora_ctx *ctx, const lora_plan_t *plan, const PlanB
         st.blk0 = st.cb0 = st.fb0 = 0;
         a.nbe_cap = g.nbe_cap;
         a.nbe = any_ad ? (int32_t)((pb.ext_rows + 15) / 16) : 0;
-        a.ks = g.ks;
+        a.ks = a.ks_ext = g.ks;
         nblk += (long)a.nbe + g.nbw;
     }
     const DecodeSet &s0 = a.set[0];  // (one projection: the launch's own fields)

@@ -4,25 +4,26 @@
 //
 //     P[n, t] = sum over a slice of  e2m1(W[n, k]) 2^(s[n, k/32] - 127)  X[t, k]
 //
-// Bound by the stream of W -- half a byte a value and a byte for 32 of them -- and, the fewer rows there are, by the chain of one
-// wave's instructions; so the weights are never taken apart by arithmetic: the hardware's conversion turns two 4-bit values and
-// their scale into two bf16 values, exactly, and the products run on 16x16x32 bf16 MFMAs.  (X in 8 bits is opened the same way,
-// exactly, when it is staged in LDS: T x K values against N x K.)
+// Bound by the stream of W -- half a byte a value and a byte for 32 of them -- by the partial tiles, and, the fewer rows there are, by the
+// chain of one wave's instructions; so the weights are never taken apart by arithmetic.  Activations in bf16: the hardware's
+// conversion turns two 4-bit values and their scale into two bf16 values, exactly, and the products run on 16x16x32 bf16
+// MFMAs.  Activations in 8 bits: block-scaled 16x16x128 MFMAs take both as they are (operand layout: mx_gemm_kernels.hip).
 //
-// A wave has 16 rows of W and a slice of SC 16-byte chunks of X (8 values each): it requests all its weights at once, 8 rows x
-// 128 bytes an instruction, and turns them into operand layout through a wave-private, XOR-swizzled LDS buffer, as the
-// decode path does for bf16.  A lane's 16 bytes there are one whole block -- row lane % 16, block 4 q + lane / 16 -- so it
-// needs one scale, and feeds four MFMAs: the j-th takes values 8 j .. 8 j + 7 of four blocks, from both sides.
-// Slices of 1024 instead of 512 values halve the partial tiles (4 bytes x T x N a slice, written and read; the weights of a slice
-// of 512 are 256 N bytes); they are taken where that still leaves a workgroup for every CU (see launch rule in mx_api.hiph).
-#include "mx_kernels.h"
+// A wave has 16 rows of W and a slice of SC chunks of 8 values: it requests all its weights at once, 8 rows x 128 bytes
+// an instruction, and turns them into operand layout through a wave-private, XOR-swizzled LDS buffer, as the decode path
+// does for bf16.  A lane's 16 bytes there are one whole block -- row lane % 16, block 4 q + lane / 16 -- so it needs one scale; in
+// bf16 they feed four MFMAs, the j-th of which takes values 8 j .. 8 j + 7 of four blocks, from both sides.
+//
+// The rows of the used A_a (bf16, slices of 512 values, X in bf16) are workgroups of their own in front of the others: their X is another
+// where the backbone's comes in 8 bits.
+#include <type_traits>
+
+#include "mx_common.hiph"
 
 namespace lora {
 namespace {
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-__device__ __forceinline__ unsigned load_u32(const void *p) { return *(const __attribute__((address_space(1))) unsigned *)p; }
 
 // A pair of bf16 values (as bits) of byte `B` / half `B` of a dword of codes.
 template <int B>
@@ -32,46 +33,58 @@ __device__ __forceinline__ unsigned open_fp4(unsigned codes, float scale) {
 __device__ __forceinline__ chunk_t open_fp4x8(unsigned codes, float scale) {
     return make_uint4(open_fp4<0>(codes, scale), open_fp4<1>(codes, scale), open_fp4<2>(codes, scale), open_fp4<3>(codes, scale));
 }
-__device__ __forceinline__ chunk_t open_fp8x8(unsigned lo, unsigned hi, float scale) {
-    return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
-                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
-                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
-                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)));
+template <typename F>
+__device__ __forceinline__ void for_pair(F &&f) {
+    f(std::integral_constant<int, 0>{});
+    f(std::integral_constant<int, 1>{});
 }
 
-// TBLK: 16-row blocks of the batch.  SC: chunks of X per slice (64 or 128).  X8: the base product's activations come in 8 bits.
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kExtChunks = 64;  // chunks of X per slice of the extension rows
+
+// X in bf16, a slice of SC chunks: requested, and put into LDS, chunk c of row t at t * SC + (c ^ (t & 15)) (zeros past T and K).
+template <int TBLK, int SC>
+struct XSlice {
+    static constexpr int MINT = kDecodeMinWaves * 64, IT = TBLK * 16 * SC / MINT;  // (with the fewest threads of a workgroup)
+    chunk_t v[IT];
+    __device__ __forceinline__ void request(const DecodeArgs &p, int kc0, int kchunks) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int idx = (int)threadIdx.x + it * (int)blockDim.x;
+            const int row = min(idx / SC, p.T - 1), c = min(kc0 + idx % SC, kchunks - 1);
+            v[it] = load_chunk(static_cast<const __bf16 *>(p.X) + (int64_t)row * p.ldx + c * 8);
+        }
+    }
+    __device__ __forceinline__ void stage(chunk_t *xs, const DecodeArgs &p, int kc0, int kchunks) const {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int idx = (int)threadIdx.x + it * (int)blockDim.x;
+            const int row = idx / SC, c = idx % SC;
+            if (idx < TBLK * 16 * SC) xs[row * SC + (c ^ (row & 15))] = keep_if(row < p.T && kc0 + c < kchunks, v[it]);
+        }
+    }
+};
+
+// TBLK: 16-row blocks of the batch.  SC: chunks of 8 values per slice of the backbone.  X8: its activations come in 8 bits.
+// (a slice of 256 chunks needs more registers than twelve waves leave)
 template <int TBLK, int SC, bool X8>
-__global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
+__global__ __launch_bounds__((SC == 256 ? kDecodeMinWaves : kDecodeMaxWaves) * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
     typedef __bf16 E;
     constexpr int XROWS = TBLK * 16;
-    constexpr int MINT = kDecodeMinWaves * 64;           // fewest threads of a workgroup
-    constexpr int XIT = XROWS * SC / MINT;               // chunk loads per thread that cover the X slice in bf16
-    constexpr int X8IT = (XROWS * SC / 2 + MINT - 1) / MINT;  // 16-byte loads that cover it in 8 bits
-    constexpr int NST = SC / 32;                         // stages of 128 bytes of a weight row
+    constexpr int NST = SC / 32;  // stages of 128 bytes of a weight row
     constexpr bool MASKED = TBLK < 8;
 
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    chunk_t *xs = reinterpret_cast<chunk_t *>(smem);  // [XROWS][SC], chunk c of row t at t * SC + (c ^ (t & 15))
-    chunk_t *wstage = xs + XROWS * SC;                // [waves][128]
-
     const DecodeArgs &p = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nthreads = blockDim.x, nw = nthreads >> 6;
     const int li = lane & 15, lg = lane >> 4;
-    const int slice = blockIdx.x % p.ks;
-    int grp = blockIdx.x / p.ks;
-    int si = 0;
-    while (si + 1 < a.n && grp >= a.w[si + 1].group0) ++si;
-    grp -= a.w[si].group0;
-    const DecodeSet &set = p.set[si];
-    // Workgroups of extension rows (rows of the used A_a) come first: their X is in bf16 whatever the others' is.
-    const bool is_ext = grp < a.ext_groups;
     const int status = p.plan.scalars[kScStatus];
-
     const int kchunks = p.K / 8;
-    const int kc0 = slice * SC;
     const int wr = lane >> 3, wc = lane & 7;  // load slot: row wr + 8 i of the block, chunk wc of a 128-byte stage
-    chunk_t *buf = wstage + wave * 128;
+    chunk_t *buf = reinterpret_cast<chunk_t *>(smem) + wave * 128;
+    chunk_t *xs = reinterpret_cast<chunk_t *>(smem) + nw * 128;
     int wdst[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -83,28 +96,15 @@ __global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(
 #pragma unroll
     for (int tb = 0; tb < TBLK; ++tb) acc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    // X slice in bf16: request, and put into LDS (zeros past T and K)
-    chunk_t xv[X8 ? (XIT > X8IT ? XIT : X8IT) : XIT];
-    auto request_x = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int it = 0; it < XIT; ++it) {
-            const int idx = tid + it * nthreads;
-            const int row = min(idx / SC, p.T - 1), c = min(kc0 + idx % SC, kchunks - 1);
-            xv[it] = load_chunk(static_cast<const E *>(p.X) + (int64_t)row * p.ldx + c * 8);
-        }
-    };
-    auto stage_x = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int it = 0; it < XIT; ++it) {
-            const int idx = tid + it * nthreads;
-            const int row = idx / SC, c = idx % SC;
-            if (idx < XROWS * SC) xs[row * SC + (c ^ (row & 15))] = keep_if(row < p.T && kc0 + c < kchunks, xv[it]);
-        }
-    };
-
-    int pblk;
+    float4 *P4;
     unsigned keep;  // token blocks whose results this lane stores, one bit each
-    if (is_ext) {
+    if ((int)blockIdx.x < a.ext_wgs) {
+        const int slice = blockIdx.x % p.ks_ext;
+        int grp = blockIdx.x / p.ks_ext;
+        const int si = grp / a.ext_groups;
+        grp -= si * a.ext_groups;
+        const DecodeSet &set = p.set[si];
+        const int kc0 = slice * kExtChunks;
         const int blk = grp * nw + wave;
         const int nrec = p.plan.scalars[kScExtTotal] >> 3;  // records of 8 ranks
         const bool valid = set.A != nullptr && blk < p.nbe && blk * 2 < nrec;
@@ -120,7 +120,8 @@ __global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(
             row_ad[tb] = -2;
             if (MASKED && tb * 16 + li < p.T) row_ad[tb] = p.plan.row_adapter[tb * 16 + li];
         }
-        request_x();
+        XSlice<TBLK, kExtChunks> xv;
+        xv.request(p, kc0, kchunks);
         const char *rowp[2];
         bool rowok[2];
 #pragma unroll
@@ -139,53 +140,70 @@ __global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(
         } else {
             keep = (TBLK - 1) * 16 + li < p.T ? (1u << TBLK) - 1u : (1u << (TBLK - 1)) - 1u;
         }
-        stage_x();
+        // (half of the block's 16 KB before X goes to LDS, whose registers the rest takes)
+        chunk_t wq[8][2];
+        auto load_w = [&](int s) __attribute__((always_inline)) {
+            const unsigned off = (unsigned)min(kc0 + s * 8 + wc, kchunks - 1) * 16u;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) wq[s][i] = load_chunk(rowp[i] + (rowok[i] ? off : 0u));
+        };
+#pragma unroll
+        for (int s = 0; s < 4; ++s) load_w(s);
+        xv.stage(xs, p, kc0, kchunks);
         lds_barrier();
         if (!valid || status != 0) return;
-        pblk = blk;
-        const int nstages = (min(SC, kchunks - kc0) + 7) >> 3;  // of 8 chunks: 64 values of A_a
-        for (int s0 = 0; s0 < nstages; s0 += 8) {
-            chunk_t wq[8][2];
+        load_w(4);
 #pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                const unsigned off = (unsigned)min(kc0 + (s0 + s) * 8 + wc, kchunks - 1) * 16u;
+        for (int s = 0; s < 8; ++s) {
+            if (s + 5 < 8) load_w(s + 5);
+            if (kc0 + s * 8 < kchunks) {  // a stage: 8 chunks, 64 values of A_a
+                buf[wdst[0]] = keep_if(rowok[0], wq[s][0]);
+                buf[wdst[1]] = keep_if(rowok[1], wq[s][1]);
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll
-                for (int i = 0; i < 2; ++i) wq[s][i] = load_chunk(rowp[i] + (rowok[i] ? off : 0u));
-            }
+                for (int h = 0; h < 2; ++h) {
+                    const chunk_t w = buf[rsrc + ((h * 4 + lg) ^ rswz)];
 #pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                if (s0 + s < nstages) {
-                    buf[wdst[0]] = keep_if(rowok[0], wq[s][0]);
-                    buf[wdst[1]] = keep_if(rowok[1], wq[s][1]);
-                    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const chunk_t w = buf[rsrc + ((h * 4 + lg) ^ rswz)];
-#pragma unroll
-                        for (int tb = 0; tb < TBLK; ++tb)
-                            Elem<E>::mma16(acc[tb], w, xs[(tb * 16 + li) * SC + (((s0 + s) * 8 + h * 4 + lg) ^ li)]);
-                    }
-                    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                    for (int tb = 0; tb < TBLK; ++tb)
+                        Elem<E>::mma16(acc[tb], w, xs[(tb * 16 + li) * kExtChunks + ((s * 8 + h * 4 + lg) ^ li)]);
                 }
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
             }
         }
+        P4 = reinterpret_cast<float4 *>(set.P) + ((int64_t)(blk * p.ks_ext + slice) * TBLK) * 64;
     } else {
-        const int blk = (grp - a.ext_groups) * nw + wave;
-        const bool valid = blk < set.nbw;
+        const int wg = (int)blockIdx.x - a.ext_wgs, slice = wg % p.ks;
+        int grp = wg / p.ks;
+        int si = 0;
+        while (si + 1 < a.n && grp >= a.w[si + 1].group0) ++si;
+        grp -= a.w[si].group0;
+        const DecodeSet &set = p.set[si];
         const MxDecodeSet &w4 = a.w[si];
+        const int kc0 = slice * SC;
+        const int blk = grp * nw + wave;
+        const bool valid = blk < set.nbw;
         const int nblocks = p.K / kMxBlock, kb0 = kc0 / 4;  // blocks of a row; the slice's first
+        keep = (TBLK - 1) * 16 + li < p.T ? (1u << TBLK) - 1u : (1u << (TBLK - 1)) - 1u;
         // ---- X first (all of it before any weights: see decode_stream_kernel) ----
-        unsigned xsc[X8 ? X8IT : 1];
+        constexpr int PC = SC / 2, SS = SC / 64;  // of X in 8 bits: 16-byte pieces and groups of 16 blocks per slice and row
+        constexpr int MINT = kDecodeMinWaves * 64, X8IT = (XROWS * PC + MINT - 1) / MINT, XSIT = (XROWS * SS + MINT - 1) / MINT;
+        chunk_t x8v[X8 ? X8IT : 1], x8s[X8 ? XSIT : 1];
+        XSlice<X8 ? 1 : TBLK, X8 ? 32 : SC> xv;
         if constexpr (X8) {
+#pragma unroll
+            for (int it = 0; it < XSIT; ++it) {
+                const int idx = tid + it * nthreads, row = min(idx / SS, p.T - 1);
+                x8s[it] = zero_chunk();
+                if (idx < XROWS * SS) x8s[it] = mx_load_scales(a.Xs + (int64_t)row * a.ldxs, slice * SS + idx % SS, nblocks);
+            }
 #pragma unroll
             for (int it = 0; it < X8IT; ++it) {
                 const int idx = tid + it * nthreads;
-                const int row = min(idx / (SC / 2), p.T - 1), c = min(kc0 / 2 + idx % (SC / 2), kchunks / 2 - 1);
-                xv[it] = load_chunk(a.Xq + (int64_t)row * a.ldxq + c * 16);
-                xsc[it] = a.Xs[(int64_t)row * a.ldxs + (c >> 1)];
+                const int row = min(idx / PC, p.T - 1), c = min(kc0 / 2 + idx % PC, kchunks / 2 - 1);
+                x8v[it] = load_chunk(a.Xq + (int64_t)row * a.ldxq + c * 16);
             }
         } else {
-            request_x();
+            xv.request(p, kc0, kchunks);
         }
         __builtin_amdgcn_s_barrier();
         // ---- all of the wave's weights: 16 rows (those past N are clamped: never read back) ----
@@ -201,99 +219,140 @@ __global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(
 #pragma unroll
             for (int i = 0; i < 2; ++i) wq[s][i] = load_chunk(rowp[i] + off);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) sq[s * 2 + q] = load_u32(srow + (min(kb0 + s * 8 + q * 4, nblocks - 1) & ~3));
+            for (int q = 0; q < 2; ++q) sq[s * 2 + q] = mx_load_u32(srow + (min(kb0 + s * 8 + q * 4, nblocks - 1) & ~3));
         }
-        keep = (TBLK - 1) * 16 + li < p.T ? (1u << TBLK) - 1u : (1u << (TBLK - 1)) - 1u;
+        // X in 8 bits in LDS: piece c of row t at t * PC + (c ^ (t & 15)); behind it the scales, in the order of the lanes (mx_transpose_scales)
+        unsigned *xsc = reinterpret_cast<unsigned *>(xs + XROWS * PC);
         if constexpr (X8) {
+#pragma unroll
+            for (int it = 0; it < XSIT; ++it) {
+                const int idx = tid + it * nthreads;
+                if (idx < XROWS * SS) reinterpret_cast<chunk_t *>(xsc)[idx] = mx_transpose_scales(x8s[it]);
+            }
 #pragma unroll
             for (int it = 0; it < X8IT; ++it) {
                 const int idx = tid + it * nthreads;
-                const int row = idx / (SC / 2), c = idx % (SC / 2) * 2;  // two chunks
-                if (idx < XROWS * (SC / 2)) {
-                    const bool ok = row < p.T && kc0 + c < kchunks;
-                    const float sc = __uint_as_float(xsc[it] << 23);
-                    xs[row * SC + (c ^ (row & 15))] = keep_if(ok, open_fp8x8(xv[it].x, xv[it].y, sc));
-                    xs[row * SC + ((c + 1) ^ (row & 15))] = keep_if(ok, open_fp8x8(xv[it].z, xv[it].w, sc));
-                }
+                const int row = idx / PC, c = idx % PC;
+                if (idx < XROWS * PC) xs[row * PC + (c ^ (row & 15))] = keep_if(row < p.T && kc0 / 2 + c < kchunks / 2, x8v[it]);
             }
         } else {
-            stage_x();
+            xv.stage(xs, p, kc0, kchunks);
         }
         lds_barrier();  // (LDS traffic only: the weight loads stay in flight across it)
         if (!valid || status != 0) return;
-        pblk = blk + p.nbe_cap;
+        unsigned xscale[TBLK];
 #pragma unroll
         for (int s = 0; s < NST; ++s) {
             if (kb0 + s * 8 >= nblocks) break;
             buf[wdst[0]] = wq[s][0];
             buf[wdst[1]] = wq[s][1];
             __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            if constexpr (X8) {
+                if (s % 2 == 0) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+                    for (int tb = 0; tb < TBLK; ++tb) xscale[tb] = xsc[((tb * 16 + li) * SS + s / 2) * 4 + lg];
+                }
+            }
+            for_pair([&](auto qc) __attribute__((always_inline)) {
+                constexpr int q = qc.value;
                 const chunk_t w = buf[rsrc + ((q * 4 + lg) ^ rswz)];
                 // (past K the codes are some of this row's, the scale 2^-127: finite, and X holds zeros there)
                 const unsigned sb = kb0 + s * 8 + q * 4 + lg < nblocks ? (sq[s * 2 + q] >> (8 * lg)) & 255u : 0u;
-                const float sc = __uint_as_float(sb << 23);
-                const unsigned wd[4] = {w.x, w.y, w.z, w.w};
+                if constexpr (X8) {
+                    const i32x8_t wo{(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const chunk_t op = open_fp4x8(wd[j], sc);
+                    for (int tb = 0; tb < TBLK; ++tb) {
+                        const chunk_t *xr = xs + (tb * 16 + li) * PC;
+                        const chunk_t u = xr[(s * 16 + q * 8 + lg) ^ li], v = xr[(s * 16 + q * 8 + 4 + lg) ^ li];
+                        const i32x8_t xo{(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w};
+                        if (s % 2 == 0)
+                            acc[tb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wo, xo, acc[tb], 4, 0, 0, (int)sb, q, (int)xscale[tb]);
+                        else
+                            acc[tb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wo, xo, acc[tb], 4, 0, 0, (int)sb, q + 2, (int)xscale[tb]);
+                    }
+                } else {
+                    const float sc = __uint_as_float(sb << 23);
+                    const unsigned wd[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                    for (int tb = 0; tb < TBLK; ++tb)
-                        Elem<E>::mma16(acc[tb], op, xs[(tb * 16 + li) * SC + ((s * 32 + q * 16 + lg * 4 + j) ^ li)]);
+                    for (int j = 0; j < 4; ++j) {
+                        const chunk_t op = open_fp4x8(wd[j], sc);
+#pragma unroll
+                        for (int tb = 0; tb < TBLK; ++tb)
+                            Elem<E>::mma16(acc[tb], op, xs[(tb * 16 + li) * SC + ((s * 32 + q * 16 + lg * 4 + j) ^ li)]);
+                    }
                 }
-            }
+            });
             __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
         }
+        P4 = reinterpret_cast<float4 *>(set.P) + (((int64_t)p.nbe_cap * p.ks_ext + (int64_t)blk * p.ks + slice) * TBLK) * 64;
     }
-    // acc[tb][e] = D[weight row blk * 16 + lg * 4 + e][token tb * 16 + li]: token-major KiB tiles, as decode_stream_kernel's
-    float4 *P4 = reinterpret_cast<float4 *>(set.P) + ((int64_t)(pblk * p.ks + slice) * TBLK) * 64 + li * 4 + lg;
+    // acc[tb][e] = D[weight row of the block lg * 4 + e][token tb * 16 + li]: token-major KiB tiles, as decode_stream_kernel's
+    P4 += li * 4 + lg;
 #pragma unroll
     for (int tb = 0; tb < TBLK; ++tb)
         if (keep >> tb & 1u) P4[tb * 64] = make_float4(acc[tb][0], acc[tb][1], acc[tb][2], acc[tb][3]);
 }
 
-template <int TBLK, int SC>
+// Bytes of LDS: the waves' buffers, and X of either kind of workgroup (its scales take 1/32 of what it does in 8 bits).
+template <int TBLK, int SC, bool X8>
 constexpr size_t mx_stream_smem(int waves) {
-    return (size_t)TBLK * 16 * SC * 16 + (size_t)waves * 2048;
+    const size_t ext = (size_t)TBLK * 16 * kExtChunks * 16, base = X8 ? (size_t)TBLK * 16 * SC * 8 + (size_t)TBLK * 16 * (SC / 64) * 16 : (size_t)TBLK * 16 * SC * 16;
+    return (size_t)waves * 2048 + (ext > base ? ext : base);
 }
+template <int TBLK, int SC, bool X8>
+constexpr bool kFits = TBLK * 16 * SC * (X8 ? 8 : 16) <= 128 * 1024 && SC <= kMxMostChunks;
 
 template <int TBLK, int SC, bool X8>
 hipError_t launch_t(const MxDecodeArgs &a0, hipStream_t stream, const KernelTimer *timer) {
-    MxDecodeArgs a = a0;
-    const int w = a.d.waves;
-    a.ext_groups = (a.d.nbe + w - 1) / w;
-    long groups = 0;
-    for (int i = 0; i < a.n; ++i) {
-        a.w[i].group0 = (int32_t)groups;
-        groups += a.ext_groups + (a.d.set[i].nbw + w - 1) / w;
+    if constexpr (kFits<TBLK, SC, X8>) {
+        MxDecodeArgs a = a0;
+        const int w = a.d.waves;
+        if (SC == 256 && w > kDecodeMinWaves) return hipErrorInvalidValue;
+        a.ext_groups = (a.d.nbe + w - 1) / w;
+        a.ext_wgs = a.n * a.ext_groups * a.d.ks_ext;
+        long groups = 0;
+        for (int i = 0; i < a.n; ++i) {
+            a.w[i].group0 = (int32_t)groups;
+            groups += (a.d.set[i].nbw + w - 1) / w;
+        }
+        const long grid = a.ext_wgs + groups * a.d.ks;
+        return launch_kernel(mx_decode_stream_kernel<TBLK, SC, X8>, dim3((unsigned)grid), dim3(w * 64), mx_stream_smem<TBLK, SC, X8>(w), stream, timer, a);
+    } else {
+        return hipErrorInvalidValue;
     }
-    const long grid = groups * a.d.ks;
-    return launch_kernel(mx_decode_stream_kernel<TBLK, SC, X8>, dim3((unsigned)grid), dim3(w * 64), mx_stream_smem<TBLK, SC>(w), stream, timer, a);
 }
-template <int TBLK, int SC>
+template <int TBLK, int SC, bool X8>
 hipError_t init_t() {
-    constexpr int smem = (int)mx_stream_smem<TBLK, SC>(kDecodeMaxWaves);
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(mx_decode_stream_kernel<TBLK, SC, false>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == hipSuccess)
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(mx_decode_stream_kernel<TBLK, SC, true>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    return e;
+    if constexpr (kFits<TBLK, SC, X8>)
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(mx_decode_stream_kernel<TBLK, SC, X8>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)mx_stream_smem<TBLK, SC, X8>(kDecodeMaxWaves));
+    return hipSuccess;
+}
+template <int TBLK, bool X8>
+hipError_t launch_x(const MxDecodeArgs &a, hipStream_t stream, const KernelTimer *timer) {
+    switch (a.d.slice_chunks) {
+        case 64:
+            return launch_t<TBLK, 64, X8>(a, stream, timer);
+        case 128:
+            return launch_t<TBLK, 128, X8>(a, stream, timer);
+        case 256:
+            return launch_t<TBLK, 256, X8>(a, stream, timer);
+        default:
+            return hipErrorInvalidValue;
+    }
 }
 template <int TBLK>
 hipError_t launch_b(const MxDecodeArgs &a, hipStream_t stream, const KernelTimer *timer) {
-    if constexpr (TBLK <= kMxWideBlocks) {
-        if (a.d.slice_chunks == 128)
-            return a.Xq ? launch_t<TBLK, 128, true>(a, stream, timer) : launch_t<TBLK, 128, false>(a, stream, timer);
-    }
-    if (a.d.slice_chunks != 64) return hipErrorInvalidValue;
-    return a.Xq ? launch_t<TBLK, 64, true>(a, stream, timer) : launch_t<TBLK, 64, false>(a, stream, timer);
+    return a.Xq ? launch_x<TBLK, true>(a, stream, timer) : launch_x<TBLK, false>(a, stream, timer);
 }
 template <int TBLK>
 hipError_t init_b() {
-    hipError_t e = init_t<TBLK, 64>();
-    if constexpr (TBLK <= kMxWideBlocks) {
-        if (e == hipSuccess) e = init_t<TBLK, 128>();
-    }
+    hipError_t e = init_t<TBLK, 64, false>();
+    if (e == hipSuccess) e = init_t<TBLK, 128, false>();
+    if (e == hipSuccess) e = init_t<TBLK, 256, false>();
+    if (e == hipSuccess) e = init_t<TBLK, 64, true>();
+    if (e == hipSuccess) e = init_t<TBLK, 128, true>();
+    if (e == hipSuccess) e = init_t<TBLK, 256, true>();
     return e;
 }
 
@@ -314,7 +373,8 @@ hipError_t init_mx_decode_kernels() {
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer) {
     const DecodeArgs &d = a.d;
     if (!(d.T > (tblk - 1) * 16 && d.T <= tblk * 16 && d.K > 0 && d.K % kMxBlock == 0 && d.nbe >= 0 && d.nbe <= d.nbe_cap && a.n >= 1 &&
-          a.n <= kMaxGemmSets && d.slice_chunks > 0 && d.ks == (d.K / 8 + d.slice_chunks - 1) / d.slice_chunks && d.waves >= kDecodeMinWaves &&
+          a.n <= kMaxGemmSets && d.slice_chunks > 0 && d.ks == (d.K / 8 + d.slice_chunks - 1) / d.slice_chunks &&
+          d.ks_ext == (d.K / 8 + kExtChunks - 1) / kExtChunks && d.waves >= kDecodeMinWaves &&
           d.waves <= kDecodeMaxWaves && (d.X != nullptr || (a.Xq != nullptr && d.nbe == 0))))
         return hipErrorInvalidValue;
     for (int i = 0; i < a.n; ++i)

@@ -32,14 +32,12 @@
 #include <type_traits>
 #include <utility>
 
-#include "mx_kernels.h"
+#include "mx_common.hiph"
 
 namespace lora {
 namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ unsigned load_u32(const void *p) { return *(const __attribute__((address_space(1))) unsigned *)p; }
 
 template <int A, typename F, int... I>
 __device__ __forceinline__ void for_impl(F &&f, std::integer_sequence<int, I...>) {
@@ -71,30 +69,6 @@ __device__ __forceinline__ void mma_scaled(f32x4_t &acc, const u32x4_t &w, const
 #else
     (void)acc, (void)w, (void)x, (void)ws, (void)xs;
 #endif
-}
-
-// The scales of 16 blocks of a row (a superstage: four stages of four blocks), as the four dwords that hold byte g of each stage.
-__device__ __forceinline__ chunk_t transpose_scales(const chunk_t &d) {
-    const unsigned a = __builtin_amdgcn_perm(d.y, d.x, 0x05010400u), b = __builtin_amdgcn_perm(d.y, d.x, 0x07030602u);
-    const unsigned c = __builtin_amdgcn_perm(d.w, d.z, 0x05010400u), e = __builtin_amdgcn_perm(d.w, d.z, 0x07030602u);
-    return make_uint4(__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u), __builtin_amdgcn_perm(e, b, 0x05040100u),
-                      __builtin_amdgcn_perm(e, b, 0x07060302u));
-}
-// Scales of blocks 16 s .. 16 s + 15 of a row of n (zeros past it).
-__device__ __forceinline__ chunk_t load_scales(const unsigned char *row, int s, int n) {
-    if (s * 16 + 16 <= n) {  // (4-byte alignment is enough)
-        typedef u32x4_t u32x4_4_t __attribute__((aligned(4)));
-        const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_4_t *)(row + s * 16);
-        return make_uint4(v.x, v.y, v.z, v.w);
-    }
-    unsigned d[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int left = n - s * 16 - i * 4;  // blocks in this dword
-        d[i] = load_u32(row + (left > 0 ? s * 16 + i * 4 : 0));
-        d[i] &= left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1u : 0u;
-    }
-    return make_uint4(d[0], d[1], d[2], d[3]);
 }
 
 // A direct load whose descriptor or offset a vector instruction may just have written (a lane read into a scalar register, which is also
@@ -245,8 +219,8 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
             set_lds_base<0>(dxs), load_to_lds_settled(Xsd, oxs, xo);
             set_lds_base<0>(dws), load_to_lds_settled(Wsd, ows, wo);
         } else {
-            xs_new = load_scales(p.Xs + b0 + (int64_t)my_row * p.ldxs + part * p.part_scales, k, nloc);
-            ws_new = load_scales(g.Ws + b0 + (int64_t)min(n0 + tid % BN, g.N - 1) * g.ldws, k, nloc);
+            xs_new = mx_load_scales(p.Xs + b0 + (int64_t)my_row * p.ldxs + part * p.part_scales, k, nloc);
+            ws_new = mx_load_scales(g.Ws + b0 + (int64_t)min(n0 + tid % BN, g.N - 1) * g.ldws, k, nloc);
         }
     };
     auto order_scales = [&](int s) __attribute__((always_inline)) {
@@ -255,10 +229,10 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         if (k * 16 + 16 <= nloc) {
 #pragma unroll
             for (int i = 0; i < (BM + BN + 255) / 256; ++i)
-                if ((BM + BN) % 256 == 0 || tid + i * 256 < BM + BN) to[tid + i * 256] = transpose_scales(sraw[tid + i * 256]);
+                if ((BM + BN) % 256 == 0 || tid + i * 256 < BM + BN) to[tid + i * 256] = mx_transpose_scales(sraw[tid + i * 256]);
         } else {
-            if (tid < BM) to[tid] = transpose_scales(xs_new);
-            if (tid < BN) to[BM + tid] = transpose_scales(ws_new);
+            if (tid < BM) to[tid] = mx_transpose_scales(xs_new);
+            if (tid < BN) to[BM + tid] = mx_transpose_scales(ws_new);
         }
     };
     request_scales(0);

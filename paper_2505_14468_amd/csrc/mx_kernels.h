@@ -53,16 +53,17 @@ struct MxDecodeSet {
     int32_t pad_;
 };
 struct MxDecodeArgs {
-    DecodeArgs d;                // set[0 .. n) in use whatever n_sets says; ks counts slices of slice_chunks
+    DecodeArgs d;                // set[0 .. n) in use whatever n_sets says; ks counts slices of slice_chunks, ks_ext those of 64
     const unsigned char *Xq;     // null: d.X
     int64_t ldxq;
     const unsigned char *Xs;
     int64_t ldxs;
     int32_t n;                   // projections
-    int32_t ext_groups;          // per projection (set by the launcher)
+    int32_t ext_groups;          // groups of workgroups for extension rows, per projection (set by the launcher)
+    int32_t ext_wgs;             // workgroups for them, which come first (set by the launcher)
     MxDecodeSet w[kMaxGemmSets];
 };
-constexpr int kMxWideBlocks = 4;  // most 16-row blocks of a batch whose X slices of 1024 values fit into LDS
+constexpr int kMxMostChunks = 256;  // longest slice, as far as X's fits into 128 KB of LDS: 16 bytes a row and chunk, or 8
 hipError_t init_mx_decode_kernels();
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
 

@@ -60,7 +60,8 @@ def test_wait_states_of_every_tile(tmp_path):
         assert not code_check.faults(code), (name, code_check.faults(code)[:3])
         prev = code_check.before(code)
         since = code_check.states_since(code, prev, lambda x: x.op.startswith("v_mfma_scale"))
-        close = [(x.text, since[i]) for i, x in enumerate(code) if not x.mfma and any(k == "a" for k, _ in x.regs) and since[i] < SCALED_TO_ACCESS]
+        accumulators = {r for x in scaled for r in x.dst}
+        close = [(x.text, since[i]) for i, x in enumerate(code) if not x.mfma and x.regs & accumulators and since[i] < SCALED_TO_ACCESS]
         assert not close, (name, close[:3])
         assert not stale_addresses(code), (name, stale_addresses(code)[:3])
 
