@@ -89,6 +89,7 @@ struct lora_ctx {
     int opt_gemm_split_k = -1;
     int opt_mx_tile = -1;
     int opt_mx_split_k = -1;
+    int opt_mx_slice = -1;
     // profiling mode: event pairs recorded tightly around each kernel
     bool prof_on = false;
     int prof_cap = 0;
@@ -1205,6 +1206,9 @@ int lora_ctx_set_option(lora_ctx *ctx, const char *name, int value) {
     } else if (!strcmp(name, "mx_tile")) {
         if (value >= kMxTileCount) return LORA_ERR_INVALID_ARG;
         ctx->opt_mx_tile = value;
+    } else if (!strcmp(name, "mx_slice")) {
+        if (value >= 0 && value != 512 && value != 1024 && value != 2048) return LORA_ERR_INVALID_ARG;
+        ctx->opt_mx_slice = value;
     } else if (!strcmp(name, "mx_split_k")) {
         if (value == 0 || value > 8) return LORA_ERR_INVALID_ARG;
         ctx->opt_mx_split_k = value;

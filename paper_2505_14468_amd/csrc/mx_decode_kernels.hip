@@ -44,9 +44,9 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 constexpr int kExtChunks = 64;  // chunks of X per slice of the extension rows
 
 // X in bf16, a slice of SC chunks: requested, and put into LDS, chunk c of row t at t * SC + (c ^ (t & 15)) (zeros past T and K).
-template <int TBLK, int SC>
+template <int TBLK, int SC, int MINT>
 struct XSlice {
-    static constexpr int MINT = kDecodeMinWaves * 64, IT = TBLK * 16 * SC / MINT;  // (with the fewest threads of a workgroup)
+    static constexpr int IT = (TBLK * 16 * SC + MINT - 1) / MINT;  // (with the fewest threads of a workgroup)
     chunk_t v[IT];
     __device__ __forceinline__ void request(const DecodeArgs &p, int kc0, int kchunks) {
 #pragma unroll
@@ -67,12 +67,12 @@ struct XSlice {
 };
 
 // TBLK: 16-row blocks of the batch.  SC: chunks of 8 values per slice of the backbone.  X8: its activations come in 8 bits.
-// (a slice of 256 chunks needs more registers than twelve waves leave)
 template <int TBLK, int SC, bool X8>
-__global__ __launch_bounds__((SC == 256 ? kDecodeMinWaves : kDecodeMaxWaves) * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
+__global__ __launch_bounds__(mx_most_waves(SC) * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
     typedef __bf16 E;
     constexpr int XROWS = TBLK * 16;
     constexpr int NST = SC / 32;  // stages of 128 bytes of a weight row
+    constexpr int MINT = mx_fewest_waves(TBLK, SC) * 64;
     constexpr bool MASKED = TBLK < 8;
 
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -120,7 +120,7 @@ __global__ __launch_bounds__((SC == 256 ? kDecodeMinWaves : kDecodeMaxWaves) * 6
             row_ad[tb] = -2;
             if (MASKED && tb * 16 + li < p.T) row_ad[tb] = p.plan.row_adapter[tb * 16 + li];
         }
-        XSlice<TBLK, kExtChunks> xv;
+        XSlice<TBLK, kExtChunks, MINT> xv;
         xv.request(p, kc0, kchunks);
         const char *rowp[2];
         bool rowok[2];
@@ -186,9 +186,9 @@ __global__ __launch_bounds__((SC == 256 ? kDecodeMinWaves : kDecodeMaxWaves) * 6
         keep = (TBLK - 1) * 16 + li < p.T ? (1u << TBLK) - 1u : (1u << (TBLK - 1)) - 1u;
         // ---- X first (all of it before any weights: see decode_stream_kernel) ----
         constexpr int PC = SC / 2, SS = SC / 64;  // of X in 8 bits: 16-byte pieces and groups of 16 blocks per slice and row
-        constexpr int MINT = kDecodeMinWaves * 64, X8IT = (XROWS * PC + MINT - 1) / MINT, XSIT = (XROWS * SS + MINT - 1) / MINT;
+        constexpr int X8IT = (XROWS * PC + MINT - 1) / MINT, XSIT = (XROWS * SS + MINT - 1) / MINT;
         chunk_t x8v[X8 ? X8IT : 1], x8s[X8 ? XSIT : 1];
-        XSlice<X8 ? 1 : TBLK, X8 ? 32 : SC> xv;
+        XSlice<X8 ? 1 : TBLK, X8 ? 32 : SC, MINT> xv;
         if constexpr (X8) {
 #pragma unroll
             for (int it = 0; it < XSIT; ++it) {
@@ -307,7 +307,7 @@ hipError_t launch_t(const MxDecodeArgs &a0, hipStream_t stream, const KernelTime
     if constexpr (kFits<TBLK, SC, X8>) {
         MxDecodeArgs a = a0;
         const int w = a.d.waves;
-        if (SC == 256 && w > kDecodeMinWaves) return hipErrorInvalidValue;
+        if (w < mx_fewest_waves(TBLK, SC) || w > mx_most_waves(SC)) return hipErrorInvalidValue;
         a.ext_groups = (a.d.nbe + w - 1) / w;
         a.ext_wgs = a.n * a.ext_groups * a.d.ks_ext;
         long groups = 0;
@@ -325,7 +325,7 @@ template <int TBLK, int SC, bool X8>
 hipError_t init_t() {
     if constexpr (kFits<TBLK, SC, X8>)
         return hipFuncSetAttribute(reinterpret_cast<const void *>(mx_decode_stream_kernel<TBLK, SC, X8>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)mx_stream_smem<TBLK, SC, X8>(kDecodeMaxWaves));
+                                   (int)mx_stream_smem<TBLK, SC, X8>(mx_most_waves(SC)));
     return hipSuccess;
 }
 template <int TBLK, bool X8>
@@ -374,8 +374,7 @@ hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t 
     const DecodeArgs &d = a.d;
     if (!(d.T > (tblk - 1) * 16 && d.T <= tblk * 16 && d.K > 0 && d.K % kMxBlock == 0 && d.nbe >= 0 && d.nbe <= d.nbe_cap && a.n >= 1 &&
           a.n <= kMaxGemmSets && d.slice_chunks > 0 && d.ks == (d.K / 8 + d.slice_chunks - 1) / d.slice_chunks &&
-          d.ks_ext == (d.K / 8 + kExtChunks - 1) / kExtChunks && d.waves >= kDecodeMinWaves &&
-          d.waves <= kDecodeMaxWaves && (d.X != nullptr || (a.Xq != nullptr && d.nbe == 0))))
+          d.ks_ext == (d.K / 8 + kExtChunks - 1) / kExtChunks && (d.X != nullptr || (a.Xq != nullptr && d.nbe == 0))))
         return hipErrorInvalidValue;
     for (int i = 0; i < a.n; ++i)
         if (!(d.set[i].N > 0 && d.set[i].nbw == (d.set[i].N + 15) / 16 && d.set[i].P != nullptr && a.w[i].Wq != nullptr && a.w[i].Ws != nullptr))

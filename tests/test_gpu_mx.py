@@ -312,6 +312,23 @@ def test_layer_normal_values(T, K, N, ranks, x8):
     _check_close(Layer(T, K, [N], ranks, x8))
 
 
+@pytest.mark.parametrize("values", [512, 1024, 2048])
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T", [1, 16, 17, 33, 64, 65, 96, 112, 128])
+def test_every_slice(T, x8, values):
+    """Decode-sized batches with each length of the backbone's slices and workgroups of 8 to 12 waves; K that ends inside a slice."""
+    c, rt, mx = _tools()
+    try:
+        c.set_option("mx_slice", values)
+        for waves, K, N in ((8, 2080, 130), (9, 4128, 200), (11, 1056, 190), (12, 3168, 410)):
+            c.set_option("decode_waves", waves)
+            c.set_option("expand_split", waves % 2)
+            _check_whole(Layer(T, K, [N], (8, 24, 64), x8, whole=True, seed=waves))
+    finally:
+        for name in ("mx_slice", "decode_waves", "expand_split"):
+            c.set_option(name, -1)
+
+
 @pytest.mark.parametrize("tile", [0, 1, 2])
 @pytest.mark.parametrize("x8", [False, True])
 @pytest.mark.parametrize("T,K,N", [(129, 32, 40), (257, 128, 300), (300, 544, 513), (200, 1600, 260), (700, 2080, 270), (513, 4128, 257)])
