@@ -180,11 +180,14 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_dequantize_kernel(MxConvertA
 
 // ---- root-mean-square norm -----------------------------------------------------------------------------------------
 // TPR threads share a row, PCS pieces of 8 values each: the row stays in registers between its sum of squares and the
-// outputs, so everything is read once.  A workgroup holds 256 / TPR rows, or one.
+// outputs, so everything is read once.  A workgroup holds NT / TPR rows.
+// Roundings: squares are exact in 64 bits and summed there, and the scale of a row is kept as two fp32 numbers, so that y is off by
+// little more than its last product's half a step -- the 8-bit output's elements next to a border would otherwise fall to
+// either side as the sum's order has it.  The 64-bit operations hide behind the loads.
 template <typename E, int TPR, int PCS>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNormArgs p) {
     constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR, WPR = TPR / 64;
-    __shared__ float part[NT / 64];
+    __shared__ double part[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = (int64_t)blockIdx.x * RPW + (RPW > 1 ? wave / WPR : 0);
     const bool mine = row < p.rows;
@@ -196,33 +199,34 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     for (int i = 0; i < PCS; ++i) load8(x + min(at + i * TPR * 8, p.K - 8), v[i]);
     if (p.R != nullptr) {
         const E *r = static_cast<const E *>(p.R) + rr * p.ldr;
+        float w[PCS][8];
 #pragma unroll
-        for (int i = 0; i < PCS; ++i) {
-            float w[8];
-            load8(r + min(at + i * TPR * 8, p.K - 8), w);
+        for (int i = 0; i < PCS; ++i) load8(r + min(at + i * TPR * 8, p.K - 8), w[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] += w[e];
-        }
+        for (int i = 0; i < PCS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] += w[i][e];
     }
-    float ss = 0.f;
+    double ss = 0.0;
 #pragma unroll
     for (int i = 0; i < PCS; ++i) {
-        float s = 0.f;
+        double s[2] = {0.0, 0.0};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += v[i][e] * v[i][e];
-        ss += at + i * TPR * 8 < p.K ? s : 0.f;
+        for (int e = 0; e < 8; ++e) s[e & 1] = __builtin_fma((double)v[i][e], (double)v[i][e], s[e & 1]);
+        ss += at + i * TPR * 8 < p.K ? s[0] + s[1] : 0.0;
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d);
     if constexpr (WPR > 1) {
         if (lane == 0) part[wave] = ss;
         __syncthreads();
-        ss = 0.f;
+        ss = 0.0;
 #pragma unroll
         for (int w = 0; w < WPR; ++w) ss += part[(RPW > 1 ? wave / WPR * WPR : 0) + w];
     }
     if (!mine) return;
-    const float inv = 1.f / sqrtf(ss / (float)p.K + p.eps);
+    const double scale = 1.0 / __builtin_sqrt(ss / (double)p.K + (double)p.eps);
+    const float hi = (float)scale, lo = __builtin_isfinite(hi) ? (float)(scale - (double)hi) : 0.f;
     // (whatever is stored is stored behind the row's last load: H and Y may be X or R)
     if (p.H != nullptr) {
         E *h = static_cast<E *>(p.H) + row * p.ldh;
@@ -232,11 +236,14 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     }
 #pragma unroll
     for (int i = 0; i < PCS; ++i) {
-        const int k = at + i * TPR * 8;
         float w[8];
-        load8(g + min(k, p.K - 8), w);
+        load8(g + min(at + i * TPR * 8, p.K - 8), w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * inv * w[e];
+        for (int e = 0; e < 8; ++e) {
+            const float t = v[i][e] * hi, rest = __builtin_fmaf(v[i][e], lo, __builtin_fmaf(v[i][e], hi, -t));
+            // (an infinity or NaN has no rest)
+            v[i][e] = __builtin_fmaf(t, w[e], __builtin_isfinite(t) ? rest * w[e] : 0.f);
+        }
     }
     if (p.Y != nullptr) {
         E *y = static_cast<E *>(p.Y) + row * p.ldy;
@@ -266,14 +273,20 @@ hipError_t launch_norm_t(const RmsNormArgs &a, hipStream_t stream, const KernelT
     return launch_kernel(rms_norm_kernel<E, TPR, PCS>, dim3((unsigned)grid), dim3(NT), 0, stream, timer, a);
 }
 
+// Threads per row by its length alone, so that a row's result does not depend on how many there are.  Measured in us with 64 / 256 / 512 / 1024
+// threads (bf16 with residual, sum, normed rows and 8-bit rows): 7500 rows of 512 9.7 / 17.6 / 32 / 58; 1000 of 1024 4.2 / 4.9 / 6.2 / 9.9;
+// 1 of 4096 5.1 / 2.7 / 2.6 / 3.2; 7500 of 4096 51 / 46 / 45 / 72 (6.1 TB/s); 1500 of 5120 14.2 with 256, 14.4, 16.6; 391 of 11008 in
+// fp32 17.0 with 256, 15.6, 15.1; 100 of 16384 7.6 with 256, 7.0, 6.8.
 template <typename E>
-hipError_t launch_norm_e(const RmsNormArgs &a, int num_cu, hipStream_t stream, const KernelTimer *timer) {
-    const int pieces = (a.K + 7) / 8;
-    (void)num_cu;
+hipError_t launch_norm_e(const RmsNormArgs &a, hipStream_t stream, const KernelTimer *timer) {
+    const int pieces = a.K / 8;
+    if (pieces <= 64) return launch_norm_t<E, 64, 1>(a, stream, timer);
+    if (pieces <= 128) return launch_norm_t<E, 64, 2>(a, stream, timer);
     if (pieces <= 256) return launch_norm_t<E, 256, 1>(a, stream, timer);
-    if (pieces <= 512) return launch_norm_t<E, 256, 2>(a, stream, timer);
-    if (pieces <= 1024) return launch_norm_t<E, 256, 4>(a, stream, timer);
-    if (pieces <= 2048) return launch_norm_t<E, 256, 8>(a, stream, timer);
+    if (pieces <= 512) return launch_norm_t<E, 512, 1>(a, stream, timer);
+    if (pieces <= 1024) return launch_norm_t<E, 512, 2>(a, stream, timer);
+    if (pieces <= 2048) return launch_norm_t<E, 512, 4>(a, stream, timer);
+    if (pieces <= 4096) return launch_norm_t<E, 1024, 4>(a, stream, timer);
     return launch_norm_t<E, 1024, 8>(a, stream, timer);
 }
 
@@ -325,9 +338,9 @@ hipError_t launch_mx_split(const MxSplitArgs &a0, hipStream_t stream, const Kern
     return launch_kernel(mx_split_kernel, dim3((unsigned)((units + kMxWaves - 1) / kMxWaves)), dim3(kMxWaves * 64), 0, stream, timer, a);
 }
 
-hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, int num_cu, hipStream_t stream, const KernelTimer *timer) {
+hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, hipStream_t stream, const KernelTimer *timer) {
     if (a.rows <= 0) return hipSuccess;
-    return dtype == 1 ? launch_norm_e<__bf16>(a, num_cu, stream, timer) : launch_norm_e<float>(a, num_cu, stream, timer);
+    return dtype == 1 ? launch_norm_e<__bf16>(a, stream, timer) : launch_norm_e<float>(a, stream, timer);
 }
 
 }  // namespace lora

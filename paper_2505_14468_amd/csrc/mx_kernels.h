@@ -41,7 +41,7 @@ struct RmsNormArgs {
     int32_t K;
     float eps;
 };
-hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, int num_cu, hipStream_t stream, const KernelTimer *timer);
+hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, hipStream_t stream, const KernelTimer *timer);
 
 // Decode-sized batches: the streaming launch of the decode path on 4-bit weights; the second launch is the decode path's own.
 struct MxDecodeSet {

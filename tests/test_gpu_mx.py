@@ -115,8 +115,8 @@ def test_conversions_with_strides_leave_the_rest_alone():
 
 
 # ---- norm ------------------------------------------------------------------------------------------------------------------
-# fp32 roundings of y: a sum of squares of at most 64 terms in a row per thread and a tree of 10 sums (each within 2^-24 of the running
-# sum, halved by the root), the square, the sum, the division, the root, its inverse and two products: 74 / 2 + 10 < 48 of them.
+# fp32 roundings of y: the sum of x and the residual, the products with the row's scale (two numbers of 24 bits) and with gamma: 3 half
+# steps; 48 are allowed, as a sum of squares in fp32 would take with 64 terms in a row per thread and a tree of 10 sums.
 NORM32 = 48 * 2.0 ** -24
 
 
@@ -161,6 +161,16 @@ def test_norm(rows, K, dtype):
                 _check_held(n.q, wy)
                 only = mx.rms_norm(c, x, g, 1e-5, residual, quantize=True, normed=False)
                 assert only.y is None and torch.equal(only.q.codes, n.q.codes) and torch.equal(only.q.scales, n.q.scales)
+
+
+def test_norm_of_a_row_does_not_depend_on_the_others():
+    c, rt, mx = _tools()
+    for K in (96, 1024, 4096, 11008):
+        x, g = torch.randn(600, K, device=c.device).bfloat16(), torch.randn(K, device=c.device).bfloat16()
+        every = mx.rms_norm(c, x, g, 1e-5, quantize=True)
+        for rows in (1, 77, 599):
+            some = mx.rms_norm(c, x[:rows], g, 1e-5, quantize=True)
+            assert torch.equal(some.y, every.y[:rows]) and torch.equal(some.q.codes, every.q.codes[:rows]) and torch.equal(some.q.scales, every.q.scales[:rows])
 
 
 def test_norm_special_rows():
