@@ -94,7 +94,8 @@ typedef struct lora_mx_linear_desc {
     int32_t flags;      /* must be 0                                                                        */
     int32_t reserved;   /* must be 0                                                                        */
     const void *X;      /* device [T, ldx] bf16.  NULL only with Xq and without adapters (tbl NULL)         */
-    int64_t ldx;        /* >= K, a multiple of 8; X smaller than 4 GiB                                      */
+    int64_t ldx;        /* >= K, a multiple of 8; X smaller than 4 GiB, and above 128 rows without Xq so is 2 T times K
+                           rounded up to whole 512                                                          */
     lora_mx_rows_t Xq;  /* [T] rows, E4M3: the base product's activations; codes == NULL: X in bf16. < 4 GiB */
     lora_mx_rows_t W;   /* [N] rows, E2M1; const, externally owned; ld_codes < 16 MiB                       */
     void *Y;            /* device [T, ldy] bf16; must not overlap any input or the workspace                */
@@ -104,14 +105,16 @@ typedef struct lora_mx_linear_desc {
     size_t workspace_bytes;
 } lora_mx_linear_desc;
 
-/* Device bytes lora_mx_linear() needs in desc->workspace (with_xq: whether Xq is given).  As for lora_linear(), and for
- * bf16 activations of more than 128 rows also 2 N K bytes: the backbone in bf16, made anew by every call.  One workspace may
- * serve calls of different shapes as long as it is big enough for each and they do not overlap in time.  0 for invalid
- * arguments. */
+/* Device bytes lora_mx_linear() needs in desc->workspace (with_xq: whether Xq is given): lora_linear()'s preferred size; above 128
+ * rows also the activations in two parts of 8 bits (bf16 ones: 2 T bytes for every K, rounded up to whole 512, and 1/32 of that), and
+ * partial sums in fp32 where the tiles alone would leave much of the chip idle.  One workspace may serve calls of different shapes
+ * as long as it is big enough for each and they do not overlap in time.  0 for invalid arguments. */
 size_t lora_mx_linear_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r_max, int32_t with_xq);
 
 /* The layer.  Products of the held values are exact and summed in fp32; the adapter term's intermediate is rounded as
- * lora_linear() says; Y is rounded once.  Returns after enqueueing launches only (it may be captured into a graph as
+ * lora_linear() says; Y is rounded once.  (Activations in bf16 of more than 128 rows are taken apart into two parts of 8 bits:
+ * exactly down to 2^-14 of the largest value of their block of 32, off by at most 2^-22 of it below.)  An infinity or a NaN among a
+ * row's activations makes that row of Y infinite or NaN, one in a block of W its column.  Returns after enqueueing launches only (it may be captured into a graph as
  * lora_linear() may).  Bitwise reproducible run to run.  Errors, all found before the first launch: INVALID_ARG, PLAN,
  * SHAPE, ALIGNMENT, WORKSPACE_TOO_SMALL; HIP if a launch fails. */
 int lora_mx_linear(lora_ctx *ctx, const lora_plan_t *plan, const lora_mx_linear_desc *desc, lora_stream_t stream);

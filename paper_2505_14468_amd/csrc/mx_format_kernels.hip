@@ -67,10 +67,15 @@ __device__ __forceinline__ unsigned codes_e2m1(const float (&v)[8], float inv) {
 
 constexpr int kMxWaves = 4;  // per workgroup
 
+// A grid of `wgs` workgroups: a dimension of a launch holds fewer than 2^32 threads.
+constexpr int64_t kGridX = 1 << 21;
+dim3 grid_of(int64_t wgs) { return wgs <= kGridX ? dim3((unsigned)wgs) : dim3((unsigned)kGridX, (unsigned)((wgs + kGridX - 1) / kGridX)); }
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * (unsigned)kGridX + blockIdx.x; }
+
 template <typename E, int FMT>
 __global__ __launch_bounds__(kMxWaves * 64) void mx_quantize_kernel(MxConvertArgs p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned unit = blockIdx.x * kMxWaves + wave, urow = unit / (unsigned)p.strips;
+    const unsigned unit = workgroup() * kMxWaves + wave, urow = unit / (unsigned)p.strips;
     const int64_t row = urow;
     if (row >= p.rows) return;
     const int k0 = (int)(unit - urow * p.strips) * kMxStrip + lane * 8;
@@ -100,7 +105,7 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_quantize_kernel(MxConvertArg
 // value's own -- down to 2^-14 of its block's largest -- and off by at most 2^-22 of that largest value below.
 __global__ __launch_bounds__(kMxWaves * 64) void mx_split_kernel(MxSplitArgs p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned unit = blockIdx.x * kMxWaves + wave, urow = unit / (unsigned)p.strips;
+    const unsigned unit = workgroup() * kMxWaves + wave, urow = unit / (unsigned)p.strips;
     if (urow >= (unsigned)p.rows) return;
     const int k0 = (int)(unit - urow * p.strips) * kMxStrip + lane * 8;
     const __bf16 *src = static_cast<const __bf16 *>(p.X) + (int64_t)urow * p.ldx;
@@ -141,7 +146,7 @@ __device__ __forceinline__ void store_values(float *dst, const float (&v)[8]) { 
 template <typename E, int FMT>
 __global__ __launch_bounds__(kMxWaves * 64) void mx_dequantize_kernel(MxConvertArgs p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned unit = blockIdx.x * kMxWaves + wave, urow = unit / (unsigned)p.strips;
+    const unsigned unit = workgroup() * kMxWaves + wave, urow = unit / (unsigned)p.strips;
     const int64_t row = urow;
     if (row >= p.rows) return;
     const int k0 = (int)(unit - urow * p.strips) * kMxStrip + lane * 8;
@@ -189,7 +194,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR, WPR = TPR / 64;
     __shared__ double part[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t row = (int64_t)blockIdx.x * RPW + (RPW > 1 ? wave / WPR : 0);
+    const int64_t row = (int64_t)workgroup() * RPW + (RPW > 1 ? wave / WPR : 0);
     const bool mine = row < p.rows;
     const int64_t rr = mine ? row : p.rows - 1;
     const int at = (RPW > 1 ? tid % TPR : tid) * 8;
@@ -269,8 +274,7 @@ template <typename E, int TPR, int PCS>
 hipError_t launch_norm_t(const RmsNormArgs &a, hipStream_t stream, const KernelTimer *timer) {
     constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
     const int64_t grid = (a.rows + RPW - 1) / RPW;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    return launch_kernel(rms_norm_kernel<E, TPR, PCS>, dim3((unsigned)grid), dim3(NT), 0, stream, timer, a);
+    return launch_kernel(rms_norm_kernel<E, TPR, PCS>, grid_of(grid), dim3(NT), 0, stream, timer, a);
 }
 
 // Threads per row by its length alone, so that a row's result does not depend on how many there are.  Measured in us with 64 / 256 / 512 / 1024
@@ -302,7 +306,7 @@ hipError_t launch_convert(const MxConvertArgs &a0, int format, int64_t ld_values
     a.strips = (a.K + kMxStrip - 1) / kMxStrip;
     const int64_t units = a.rows * a.strips;  // (fewer than 2^31: the caller has checked)
     if (units <= 0) return hipSuccess;
-    return launch(a, dim3((unsigned)((units + kMxWaves - 1) / kMxWaves)));
+    return launch(a, grid_of((units + kMxWaves - 1) / kMxWaves));
 }
 
 }  // namespace
@@ -335,7 +339,7 @@ hipError_t launch_mx_split(const MxSplitArgs &a0, hipStream_t stream, const Kern
     const int64_t units = (int64_t)a.rows * a.strips;
     if (units <= 0) return hipSuccess;
     if (units > INT32_MAX || a.part_bytes % 512 || a.part_bytes < a.K || a.part_scales < a.part_bytes / kMxBlock) return hipErrorInvalidValue;
-    return launch_kernel(mx_split_kernel, dim3((unsigned)((units + kMxWaves - 1) / kMxWaves)), dim3(kMxWaves * 64), 0, stream, timer, a);
+    return launch_kernel(mx_split_kernel, grid_of((units + kMxWaves - 1) / kMxWaves), dim3(kMxWaves * 64), 0, stream, timer, a);
 }
 
 hipError_t launch_rms_norm(const RmsNormArgs &a, int dtype, hipStream_t stream, const KernelTimer *timer) {

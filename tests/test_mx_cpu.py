@@ -156,7 +156,7 @@ def test_workspace_bytes():
     for T in (1, 128, 129, 5000):
         for xq in (0, 1):
             least = B.lora_linear_workspace_bytes_preferred(T, 4096, 1000, 16, B.LORA_DTYPE_BF16)
-            assert f(T, 4096, 1000, 16, xq) >= least + (2 * 4096 * 1000 if T > 128 and not xq else 0)
+            assert f(T, 4096, 1000, 16, xq) >= least + (2 * T * (4096 + 128) if T > 128 and not xq else 0)  # (X as two parts of 8 bits, with scales)
             assert f(T, 4096, 1000, 16, xq) % 256 == 0
 
 
@@ -198,3 +198,77 @@ def test_oracle_norm_and_layer_closed_forms():
     X, W, A, Bw = np.array([[1.0, 2.0], [3.0, 4.0]]), np.array([[1.0, -1.0]]), [np.array([[1.0, 1.0]])], [np.array([[2.0]])]
     Y, S, D = ref.linear(X, W, X, [-1, 0], A, Bw, [0.5])
     assert np.array_equal(Y, [[-1.0], [-1.0 + 0.5 * 7 * 2]]) and np.array_equal(S, [[3.0], [14.0]]) and np.array_equal(D, [[0.0], [7.0]])
+
+
+# ---- what is launched, on a stand-in HIP runtime ----------------------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    import fake_hip
+    return fake_hip.build(tmp_path_factory.mktemp("fake_hip"))
+
+
+def test_grids_of_many_rows_stay_within_what_a_launch_takes(fake):
+    import fake_hip
+    fake_hip.run(fake, """
+        from paper_2505_14468_amd import mx
+        AT = [(i + 1) << 44 for i in range(8)]
+        rows = 2 ** 30
+        q = lambda fmt, ld: mx.lora_mx_rows_t(AT[1], ld, AT[2], 4, fmt, 0)
+        calls = [lambda n: mx.lora_rms_norm(ctx, mx.lora_rms_norm_desc(1, 32, n, 1e-5, 0, AT[0], 32, None, 0, AT[3], None, 0, AT[4], 32, q(1, 32)), 0),
+                 lambda n: mx.lora_rms_norm(ctx, mx.lora_rms_norm_desc(0, 4096, n // 64, 1e-5, 0, AT[0], 4096, None, 0, AT[3], None, 0, AT[4], 4096,
+                                                                       mx.lora_mx_rows_t()), 0),
+                 lambda n: mx.lora_mx_quantize(ctx, mx.lora_mx_convert_desc(1, 32, n, AT[0], 32, q(0, 16)), 0),
+                 lambda n: mx.lora_mx_dequantize(ctx, mx.lora_mx_convert_desc(0, 32, n, AT[0], 40, q(1, 32)), 0)]
+        for call in calls:
+            areas = []
+            for n in (rows, 64):
+                F.fake_reset()
+                call(n)
+                (name, grid, block), = launched()
+                assert all(g * b < 2 ** 32 and g < 2 ** 31 for g, b in zip(grid, block)), (name, grid, block)
+                areas.append(grid[0] * grid[1] * block[0])
+            assert areas[0] >= rows // 64 * 64 and areas[1] <= 64 * 512, areas
+    """)
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_captured_layers_have_room_for_every_batch_of_the_same_sizes(fake, T):
+    """As the bf16 layer's: the grids of a captured call do not depend on what the batch at capture used."""
+    import fake_hip
+    fake_hip.run(fake, f"""
+        from paper_2505_14468_amd import mx
+        T, K = {T}, 1056
+        lens = np.diff(np.linspace(0, T, 33).astype(int))
+        one = make_plan(np.zeros(32, int), lens, np.where(np.arange(32) == 0, 8, 64), r_max=64)
+        many = make_plan(np.arange(32), lens, np.full(32, 64), r_max=64)
+
+        def desc(plan, N, x8):
+            d = make_desc(plan, K, N)
+            size = mx.lora_mx_linear_workspace_bytes(T, K, N, 64, x8)
+            rows = lambda n, w, fmt: mx.lora_mx_rows_t(mem(n * w), w, mem(n * 36), 36, fmt, 0)
+            m = mx.lora_mx_linear_desc(K, N, 0, 0, d.X, d.ldx, rows(T, K, 1) if x8 else mx.lora_mx_rows_t(), rows(N, K // 2, 0), d.Y, d.ldy, d.tbl,
+                                       mem(size), size)
+            m._keep = d
+            return m
+
+        def grids(plan):
+            out = []
+            for x8 in (0, 1):
+                d = [desc(plan, n, x8) for n in (96, 200)]
+                d[1].X, d[1].Xq = d[0].X, d[0].Xq
+                for call in (lambda: mx.lora_mx_linear(ctx, plan, d[0], 0), lambda: mx.lora_mx_linear_multi(ctx, plan, d, 0)):
+                    F.fake_reset()
+                    say("capturing", capturing)
+                    call()
+                    assert F.fake_launches() > 0
+                    out.append(launched())
+            return out
+
+        capturing = 1
+        assert grids(one) == grids(many)
+        captured = grids(one)
+        capturing = 0
+        area = lambda launches: sum(g[0] * g[1] * g[2] * b[0] for _, g, b in launches)
+        assert all(area(e) <= area(c) for e, c in zip(grids(one), captured))
+    """)
