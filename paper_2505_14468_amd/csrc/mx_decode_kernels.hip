@@ -43,7 +43,7 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kExtChunks = 64;  // chunks of X per slice of the extension rows
 
-// X in bf16, a slice of SC chunks: requested, and put into LDS, chunk c of row t at t * SC + (c ^ (t & 15)) (zeros past T and K).
+// X in bf16, a slice of SC chunks: requested, and put into LDS, chunk c of row t at t * SC + (c ^ mx_row_swizzle(t)) (zeros past T and K).
 template <int TBLK, int SC, int MINT>
 struct XSlice {
     static constexpr int IT = (TBLK * 16 * SC + MINT - 1) / MINT;  // (with the fewest threads of a workgroup)
@@ -61,7 +61,7 @@ struct XSlice {
         for (int it = 0; it < IT; ++it) {
             const int idx = (int)threadIdx.x + it * (int)blockDim.x;
             const int row = idx / SC, c = idx % SC;
-            if (idx < TBLK * 16 * SC) xs[row * SC + (c ^ (row & 15))] = keep_if(row < p.T && kc0 + c < kchunks, v[it]);
+            if (idx < TBLK * 16 * SC) xs[row * SC + (c ^ mx_row_swizzle(row))] = keep_if(row < p.T && kc0 + c < kchunks, v[it]);
         }
     }
 };
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(mx_most_waves(SC) * 64) void mx_decode_stream_kerne
         const int row = wr + 8 * i;
         wdst[i] = row * 8 + (wc ^ ((row >> 1) & 7));
     }
-    const int rsrc = li * 8, rswz = (li >> 1) & 7;
+    const int rsrc = li * 8, rswz = (li >> 1) & 7, lsw = mx_row_swizzle(li);
     f32x4_t acc[TBLK];
 #pragma unroll
     for (int tb = 0; tb < TBLK; ++tb) acc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(mx_most_waves(SC) * 64) void mx_decode_stream_kerne
                     const chunk_t w = buf[rsrc + ((h * 4 + lg) ^ rswz)];
 #pragma unroll
                     for (int tb = 0; tb < TBLK; ++tb)
-                        Elem<E>::mma16(acc[tb], w, xs[(tb * 16 + li) * kExtChunks + ((s * 8 + h * 4 + lg) ^ li)]);
+                        Elem<E>::mma16(acc[tb], w, xs[(tb * 16 + li) * kExtChunks + ((s * 8 + h * 4 + lg) ^ lsw)]);
                 }
                 __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
             }
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(mx_most_waves(SC) * 64) void mx_decode_stream_kerne
                         const chunk_t op = open_fp4x8(wd[j], sc);
 #pragma unroll
                         for (int tb = 0; tb < TBLK; ++tb)
-                            Elem<E>::mma16(acc[tb], op, xs[(tb * 16 + li) * SC + ((s * 32 + q * 16 + lg * 4 + j) ^ li)]);
+                            Elem<E>::mma16(acc[tb], op, xs[(tb * 16 + li) * SC + ((s * 32 + q * 16 + lg * 4 + j) ^ lsw)]);
                     }
                 }
             });

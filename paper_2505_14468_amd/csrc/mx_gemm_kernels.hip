@@ -51,7 +51,7 @@ __device__ __forceinline__ void for_each(F &&f) {
 // LDS position (in 16-byte pieces) of piece c of row r: rows of X of 8 pieces, rows of W of 4, two to a line of 8.  16 rows of one
 // piece column, as an operand read takes them, then lie in 16 different quarters of the banks.
 __device__ __forceinline__ int x_at(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
-__device__ __forceinline__ int w_at(int r, int c) { return (r >> 1) * 8 + ((((r & 1) << 2) | c) ^ ((r >> 2) & 3)); }
+__device__ __forceinline__ int w_at(int r, int c) { return (r >> 1) * 8 + ((((r & 1) << 2) | c) ^ mx_quarter((r >> 2) & 3)); }
 
 // acc += W X on byte S of the scale registers, in place.  Assembly for the reason that Elem<>::mma_step gives: the accumulators
 // stay in their registers; mma_settle keeps the distance to whatever touches them next.
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
 #pragma unroll
     for (int i = 0; i < GW; ++i) {
         const int row = rw0 + i * 16 + 2 * (lane >> 3) + ((lane & 7) >> 2);
-        ow[i] = (unsigned)((int64_t)(min(n0 + row, g.N - 1) - n0) * g.ldwq) + (unsigned)((lane & 3) ^ ((row >> 2) & 3)) * 16u;
+        ow[i] = (unsigned)((int64_t)(min(n0 + row, g.N - 1) - n0) * g.ldwq) + (unsigned)((lane & 3) ^ mx_quarter((row >> 2) & 3)) * 16u;
     }
     const unsigned char *Xb = p.Xq + (int64_t)b0 * 32, *Wb = g.Wq + (int64_t)n0 * g.ldwq + b0 * 16;
     const int64_t x_row = PARTS == 2 ? 2 * (int64_t)p.part_bytes : (int64_t)nblocks * 32;  // bytes of a row of X in use
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
         }
 #pragma unroll
         for (int i = 0; i < GW; ++i) {
-            const int row = rw0 + i * 16 + 2 * (lane >> 3) + ((lane & 7) >> 2), j = j0 + ((lane & 3) ^ ((row >> 2) & 3)) * 8;
+            const int row = rw0 + i * 16 + 2 * (lane >> 3) + ((lane & 7) >> 2), j = j0 + ((lane & 3) ^ mx_quarter((row >> 2) & 3)) * 8;
             ow[i] = j < r ? (unsigned)(min(n0 + row, g.N - 1) - n0) * (unsigned)(r * 2) + (unsigned)j * 2u : ~15u;
         }
         return span;
