@@ -174,8 +174,8 @@ int lora_ctx_destroy(lora_ctx *ctx);
  * 4-bit backbone (lora_mx.h): "mx_tile" (0 tile 256x256, 1 128x256, 2 128x128),
  * "mx_split_k" (stretches of K, 1 to 8, as far as the workspace has room for
  * their sums; several projections in one call: 1), "mx_slice" (up to 128 rows:
- * values of K per slice of the backbone, 512, 1024 or 2048, as far as LDS has
- * room for the rows).  value < 0
+ * values of K per slice of the backbone, 512 or 1024, as far as LDS has room for
+ * the rows).  value < 0
  * restores the built-in choice.  Results never depend on them beyond fp32
  * summation order and, for "expand_split" on the decode path, the rounding of
  * V to bf16.  Not thread-safe against concurrent calls on the same ctx.

@@ -1207,7 +1207,7 @@ int lora_ctx_set_option(lora_ctx *ctx, const char *name, int value) {
         if (value >= kMxTileCount) return LORA_ERR_INVALID_ARG;
         ctx->opt_mx_tile = value;
     } else if (!strcmp(name, "mx_slice")) {
-        if (value >= 0 && value != 512 && value != 1024 && value != 2048) return LORA_ERR_INVALID_ARG;
+        if (value >= 0 && value != 512 && value != 1024) return LORA_ERR_INVALID_ARG;
         ctx->opt_mx_slice = value;
     } else if (!strcmp(name, "mx_split_k")) {
         if (value == 0 || value > 8) return LORA_ERR_INVALID_ARG;

@@ -68,7 +68,7 @@ struct XSlice {
 
 // TBLK: 16-row blocks of the batch.  SC: chunks of 8 values per slice of the backbone.  X8: its activations come in 8 bits.
 template <int TBLK, int SC, bool X8>
-__global__ __launch_bounds__(mx_most_waves(SC) * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
+__global__ __launch_bounds__(kDecodeMaxWaves * 64) void mx_decode_stream_kernel(MxDecodeArgs a) {
     typedef __bf16 E;
     constexpr int XROWS = TBLK * 16;
     constexpr int NST = SC / 32;  // stages of 128 bytes of a weight row
@@ -307,7 +307,7 @@ hipError_t launch_t(const MxDecodeArgs &a0, hipStream_t stream, const KernelTime
     if constexpr (kFits<TBLK, SC, X8>) {
         MxDecodeArgs a = a0;
         const int w = a.d.waves;
-        if (w < mx_fewest_waves(TBLK, SC) || w > mx_most_waves(SC)) return hipErrorInvalidValue;
+        if (w < mx_fewest_waves(TBLK, SC) || w > kDecodeMaxWaves) return hipErrorInvalidValue;
         a.ext_groups = (a.d.nbe + w - 1) / w;
         a.ext_wgs = a.n * a.ext_groups * a.d.ks_ext;
         long groups = 0;
@@ -325,7 +325,7 @@ template <int TBLK, int SC, bool X8>
 hipError_t init_t() {
     if constexpr (kFits<TBLK, SC, X8>)
         return hipFuncSetAttribute(reinterpret_cast<const void *>(mx_decode_stream_kernel<TBLK, SC, X8>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)mx_stream_smem<TBLK, SC, X8>(mx_most_waves(SC)));
+                                   (int)mx_stream_smem<TBLK, SC, X8>(kDecodeMaxWaves));
     return hipSuccess;
 }
 template <int TBLK, bool X8>
@@ -335,8 +335,6 @@ hipError_t launch_x(const MxDecodeArgs &a, hipStream_t stream, const KernelTimer
             return launch_t<TBLK, 64, X8>(a, stream, timer);
         case 128:
             return launch_t<TBLK, 128, X8>(a, stream, timer);
-        case 256:
-            return launch_t<TBLK, 256, X8>(a, stream, timer);
         default:
             return hipErrorInvalidValue;
     }
@@ -349,10 +347,8 @@ template <int TBLK>
 hipError_t init_b() {
     hipError_t e = init_t<TBLK, 64, false>();
     if (e == hipSuccess) e = init_t<TBLK, 128, false>();
-    if (e == hipSuccess) e = init_t<TBLK, 256, false>();
     if (e == hipSuccess) e = init_t<TBLK, 64, true>();
     if (e == hipSuccess) e = init_t<TBLK, 128, true>();
-    if (e == hipSuccess) e = init_t<TBLK, 256, true>();
     return e;
 }
 

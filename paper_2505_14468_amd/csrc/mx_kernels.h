@@ -63,12 +63,11 @@ struct MxDecodeArgs {
     int32_t ext_wgs;             // workgroups for them, which come first (set by the launcher)
     MxDecodeSet w[kMaxGemmSets];
 };
-constexpr int kMxMostChunks = 256;  // longest slice, as far as X's fits into 128 KB of LDS: 16 bytes a row and chunk, or 8
-// Waves per workgroup, by the batch's 16-row blocks and the slice: 8 to 12.  A slice of 256 chunks takes more registers than twelve leave
-// (168); with one of 128 and 64 rows or more it is X on its way to LDS that does, of which eleven waves have less each (64 rows 4096
-// -> 11008 with seven registers spilled: 19.2 us).
-constexpr int mx_most_waves(int slice_chunks) { return slice_chunks == 256 ? 8 : 12; }
-constexpr int mx_fewest_waves(int tblk, int slice_chunks) { return slice_chunks == 128 && tblk >= 4 ? 11 : 8; }
+// Slices of 64 or 128 chunks, the longer as far as X's fits into 128 KB of LDS (16 bytes a row and chunk, or 8).  Workgroups of at least
+// eleven waves where X on its way to LDS would take more registers than twelve leave (168; 64 rows 4096 -> 11008 with seven
+// of them spilled: 19.2 us, 16.0 without).
+constexpr int kMxMostChunks = 128;
+constexpr int mx_fewest_waves(int tblk, int slice_chunks) { return tblk >= 7 || (slice_chunks == 128 && tblk >= 4) ? 11 : kDecodeMinWaves; }
 hipError_t init_mx_decode_kernels();
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
 
