@@ -171,8 +171,8 @@ int lora_ctx_destroy(lora_ctx *ctx);
  * by the separate expand kernel or the decode path's finishing kernel with
  * every workspace of the preferred size), "gemm_split_k" (0: never split the
  * tiled GEMM along K), "shrink_rank_block" (8 / 16 / 32 / 64); of the layer on a
- * 4-bit backbone (lora_mx.h): "mx_tile" (0 tile 256x256, 1 128x256, 2 128x128),
- * "mx_split_k" (stretches of K, 1 to 8, as far as the workspace has room for
+ * 4-bit backbone (lora_mx.h): "mx_tile" (0 tile 256x256, 1 128x256, 2 128x128,
+ * 3 256x256 with 128x256 for a last 128 rows or fewer), "mx_split_k" (stretches of K, 1 to 8, as far as the workspace has room for
  * their sums; several projections in one call: 1), "mx_slice" (up to 128 rows:
  * values of K per slice of the backbone, 512 or 1024, as far as LDS has room for
  * the rows).  value < 0

@@ -93,8 +93,9 @@ struct MxTile {
     static_assert(NBT % 2 == 0 && NBN % 2 == 0 && HT >= 1 && HN >= 1 && GX >= 1 && GW >= 1 && BM + BN <= 2 * NT && BM <= NT && BN <= NT, "tile shape");
 };
 
+// One tile: rows from m0 on (in slot order), column tile pn of all projections'.
 template <int BM, int BN, int PARTS, bool SPLIT>
-__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m, int tiles_n, int group_m) {
+__device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs &p, int m0, int pn) {
     typedef MxTile<BM, BN> M;
     typedef __bf16 E;
     constexpr int NBT = M::NBT, NBN = M::NBN, HT = M::HT, HN = M::HN, GX = M::GX, GW = M::GW, D = M::D;
@@ -109,19 +110,10 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
     int *scnt = srow + BM;                                                       // segments found per wave
     unsigned char *use_d = reinterpret_cast<unsigned char *>(scnt + 4);          // tile row takes its adapter term from D
 
-    // ---- workgroup -> tile: consecutive ids go round the 8 XCDs, each walks a contiguous, M-grouped range ----
-    const int total = tiles_m * tiles_n;
-    const int per_xcd = (total + 7) >> 3;
-    const int lin = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (lin >= total) return;
-    const int width = group_m * tiles_n;
-    const int first_m = lin / width * group_m;
-    const int gsz = min(tiles_m - first_m, group_m);
-    const int pm = first_m + (lin % width) % gsz, pn = (lin % width) / gsz;
     int si = 0;
     while (si + 1 < p.n_sets && pn >= p.set[si + 1].tile0) ++si;
     const MxGemmSet g = p.set[si];
-    const int m0 = pm * BM, n0 = (pn - g.tile0) * BN;
+    const int n0 = (pn - g.tile0) * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wn0 = (wave & 1) * M::WTN, wm0 = (wave >> 1) * M::WTM;
     const int lr = lane & 15, lq = lane >> 4;
@@ -551,6 +543,37 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m,
     }
 }
 
+// Workgroup -> tile: consecutive ids go round the 8 XCDs, each walks a contiguous range in groups of group_m row tiles.
+__device__ __forceinline__ bool tile_of(int id, int tiles_m, int tiles_n, int group_m, int *pm, int *pn) {
+    const int total = tiles_m * tiles_n;
+    const int per_xcd = (total + 7) >> 3;
+    const int lin = (id & 7) * per_xcd + (id >> 3);
+    if (lin >= total) return false;
+    const int width = group_m * tiles_n;
+    const int first_m = lin / width * group_m;
+    const int gsz = min(tiles_m - first_m, group_m);
+    *pm = first_m + (lin % width) % gsz;
+    *pn = (lin % width) / gsz;
+    return true;
+}
+
+template <int BM, int BN, int PARTS, bool SPLIT>
+__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs p, int tiles_m, int tiles_n, int group_m) {
+    int pm, pn;
+    if (tile_of(blockIdx.x, tiles_m, tiles_n, group_m, &pm, &pn)) mx_gemm_tile<BM, BN, PARTS, SPLIT>(p, pm * BM, pn);
+}
+
+// 256 x 256 tiles, and behind them tiles of 128 x 256 for the last, at most 128 rows: the chip's last round is then that much shorter, or
+// there is none (7500 rows 4096 -> 11008: 1247 tiles and 43 of half the work in five rounds, where 1290 take a sixth for ten of them).
+template <int PARTS>
+__global__ __launch_bounds__(256) void mx_gemm_kernel_mixed(MxGemmArgs p, int tiles_m, int tiles_n, int group_m, int first_small) {
+    int pm, pn;
+    if ((int)blockIdx.x >= first_small)
+        mx_gemm_tile<128, 256, PARTS, false>(p, tiles_m * 256, (int)blockIdx.x - first_small);
+    else if (tile_of(blockIdx.x, tiles_m, tiles_n, group_m, &pm, &pn))
+        mx_gemm_tile<256, 256, PARTS, false>(p, pm * 256, pn);
+}
+
 template <int BM, int BN, int PARTS, bool SPLIT>
 hipError_t launch_s(const MxGemmArgs &a0, hipStream_t stream, const KernelTimer *timer) {
     MxGemmArgs a = a0;
@@ -584,12 +607,33 @@ hipError_t init_t() {
     return hipSuccess;
 }
 
+constexpr size_t kMixedSmem = MxTile<128, 256>::smem > MxTile<256, 256>::smem ? MxTile<128, 256>::smem : MxTile<256, 256>::smem;
+template <int PARTS>
+hipError_t launch_mixed(const MxGemmArgs &a0, hipStream_t stream, const KernelTimer *timer) {
+    MxGemmArgs a = a0;
+    const int tiles_m = a.T / 256, rest = a.T % 256;
+    if (tiles_m < 1 || rest < 1 || rest > 128 || a.split_k > 1) return hipErrorInvalidValue;
+    int tiles_n = 0;
+    for (int i = 0; i < a.n_sets; ++i) {
+        a.set[i].tile0 = tiles_n;
+        tiles_n += (a.set[i].N + 255) / 256;
+    }
+    const long big = ((long)tiles_m * tiles_n + 7) / 8 * 8;
+    return launch_kernel(mx_gemm_kernel_mixed<PARTS>, dim3((unsigned)(big + tiles_n)), dim3(256), kMixedSmem, stream, timer, a, tiles_m, tiles_n, 8, (int)big);
+}
+hipError_t init_mixed() {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(mx_gemm_kernel_mixed<1>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMixedSmem);
+    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(mx_gemm_kernel_mixed<2>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMixedSmem);
+    return e;
+}
+
 }  // namespace
 
 hipError_t init_mx_gemm_kernels() {
     hipError_t e = init_t<256, 256>();
     if (e == hipSuccess) e = init_t<128, 256>();
     if (e == hipSuccess) e = init_t<128, 128>();
+    if (e == hipSuccess) e = init_mixed();
     return e;
 }
 
@@ -610,6 +654,8 @@ hipError_t launch_mx_gemm(const MxGemmArgs &a, int variant, hipStream_t stream, 
             return launch_t<128, 256>(a, stream, timer);
         case kMxTile128x128:
             return launch_t<128, 128>(a, stream, timer);
+        case kMxTileMixed:
+            return a.parts == 2 ? launch_mixed<2>(a, stream, timer) : launch_mixed<1>(a, stream, timer);
         default:
             return hipErrorInvalidValue;
     }

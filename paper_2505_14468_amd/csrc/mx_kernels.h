@@ -72,7 +72,7 @@ hipError_t init_mx_decode_kernels();
 hipError_t launch_mx_decode_stream(const MxDecodeArgs &a, int tblk, hipStream_t stream, const KernelTimer *timer);
 
 // More rows: tiles on 4-bit weights and 8-bit activations.
-enum MxTileVariant { kMxTile256x256 = 0, kMxTile128x256 = 1, kMxTile128x128 = 2, kMxTileCount };
+enum MxTileVariant { kMxTile256x256 = 0, kMxTile128x256 = 1, kMxTile128x128 = 2, kMxTileMixed = 3, kMxTileCount };  // (mixed: 256x256, and 128x256 for the last rows)
 struct MxGemmSet {
     const unsigned char *Wq;
     int64_t ldwq;

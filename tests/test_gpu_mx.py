@@ -339,7 +339,7 @@ def test_every_slice(T, x8, values):
             c.set_option(name, -1)
 
 
-@pytest.mark.parametrize("tile", [0, 1, 2])
+@pytest.mark.parametrize("tile", [0, 1, 2, 3])
 @pytest.mark.parametrize("x8", [False, True])
 @pytest.mark.parametrize("T,K,N", [(129, 32, 40), (257, 128, 300), (300, 544, 513), (200, 1600, 260), (700, 2080, 270), (513, 4128, 257)])
 def test_every_tile_and_split(T, K, N, x8, tile):
@@ -362,7 +362,7 @@ def test_every_tile_and_split(T, K, N, x8, tile):
             c.set_option(name, -1)
 
 
-@pytest.mark.parametrize("tile", [0, 1, 2])
+@pytest.mark.parametrize("tile", [0, 1, 2, 3])
 def test_many_segments_in_a_tile(tile):
     """A row to a segment, and segments of every length, with the whole adapter term in the tile."""
     c, rt, mx = _tools()

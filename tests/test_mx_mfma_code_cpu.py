@@ -53,7 +53,7 @@ def test_wait_states_of_every_tile(tmp_path):
             obj = tmp_path / f"object_{k}"
             obj.write_bytes(data)
             found.update(_kernels(obj))
-    assert len(found) == 12  # three tiles, one or two parts, whole or split
+    assert len(found) == 14  # three tiles, one or two parts, whole or split; two of two tiles
     for name, code in found.items():
         scaled = [x for x in code if x.op.startswith("v_mfma_scale")]
         assert len(scaled) >= 64 and sum(x.lds_load for x in code) >= 6, name
