@@ -81,7 +81,7 @@ typedef struct lora_rms_norm_desc {
 } lora_rms_norm_desc;
 
 /* h = X + R (X alone without R), in fp32;  y = h / sqrt(mean(h^2) + eps) * gamma, the mean in 64 bits; H and Y are h and y rounded
- * once, q is lora_mx_quantize() of y in fp32.  At least one of H, Y and q; outputs may not overlap each other, gamma, or -- but
+ * once, q is what lora_mx_quantize() would make of y before any rounding.  At least one of H, Y and q; outputs may not overlap each other, gamma, or -- but
  * for the two cases above -- the inputs.  Rows are independent, and a row's result does not depend on the others.
  * Asynchronous on `stream`; no-op for 0 rows.  Errors: INVALID_ARG, SHAPE, ALIGNMENT; HIP if the launch fails. */
 int lora_rms_norm(lora_ctx *ctx, const lora_rms_norm_desc *desc, lora_stream_t stream);

@@ -186,9 +186,20 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_dequantize_kernel(MxConvertA
 // ---- root-mean-square norm -----------------------------------------------------------------------------------------
 // TPR threads share a row, PCS pieces of 8 values each: the row stays in registers between its sum of squares and the
 // outputs, so everything is read once.  A workgroup holds NT / TPR rows.
-// Roundings: squares are exact in 64 bits and summed there, and the scale of a row is kept as two fp32 numbers, so that y is off by
-// little more than its last product's half a step -- the 8-bit output's elements next to a border would otherwise fall to
-// either side as the sum's order has it.  The 64-bit operations hide behind the loads.
+// Roundings: squares are exact in 64 bits and summed there, and the scale of a row is kept as two fp32 numbers, so that fp32's y is off by
+// little more than its last product's half a step.  The narrower outputs are rounded from more bits than that (to_odd): from fp32's y one
+// element in 2^21 would fall to the wrong side of a border between two 8-bit values.  The 64-bit sums hide
+// behind the loads; rounding once costs 46.4 -> 47.1 us at 7500 rows of 4096, 14.9 -> 16.5 at 1500 of 5120.
+
+// `y` with what is missing from it folded into its last bit ("round to odd"): a later rounding to at most 22 bits then gives what rounding
+// y + rest once would give, because a border between such values has an even last bit, which only an exact y keeps.
+// |rest| is at most half a step of y: towards zero if it points there, then the last bit set.  Nothing is folded in where rest is not a
+// normal number: y is exact, not finite, or below 2^-102.
+__device__ __forceinline__ float to_odd(float y, float rest) {
+    const int bits = __float_as_int(y), back = (bits ^ __float_as_int(rest)) >> 31;
+    return __builtin_amdgcn_classf(rest, 0x108) ? __int_as_float((bits + back) | 1) : y;
+}
+
 template <typename E, int TPR, int PCS>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNormArgs p) {
     constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR, WPR = TPR / 64;
@@ -204,13 +215,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     for (int i = 0; i < PCS; ++i) load8(x + min(at + i * TPR * 8, p.K - 8), v[i]);
     if (p.R != nullptr) {
         const E *r = static_cast<const E *>(p.R) + rr * p.ldr;
-        float w[PCS][8];
+        constexpr int AHEAD = PCS < 4 ? PCS : 4;  // (eight pieces of both do not fit the registers of 1024 threads)
 #pragma unroll
-        for (int i = 0; i < PCS; ++i) load8(r + min(at + i * TPR * 8, p.K - 8), w[i]);
+        for (int j = 0; j < PCS; j += AHEAD) {
+            float w[AHEAD][8];
 #pragma unroll
-        for (int i = 0; i < PCS; ++i)
+            for (int i = 0; i < AHEAD; ++i) load8(r + min(at + (j + i) * TPR * 8, p.K - 8), w[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] += w[i][e];
+            for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[j + i][e] += w[i][e];
+            if constexpr (AHEAD < PCS)
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(v[j + i][e])::"memory");
+        }
     }
     double ss = 0.0;
 #pragma unroll
@@ -243,14 +263,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     for (int i = 0; i < PCS; ++i) {
         float w[8];
         load8(g + min(at + i * TPR * 8, p.K - 8), w);
+        float y32[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float t = v[i][e] * hi, rest = __builtin_fmaf(v[i][e], lo, __builtin_fmaf(v[i][e], hi, -t));
+            const float t = v[i][e] * hi;
             // (an infinity or NaN has no rest)
-            v[i][e] = __builtin_fmaf(t, w[e], __builtin_isfinite(t) ? rest * w[e] : 0.f);
+            const float rest = __builtin_isfinite(t) ? __builtin_fmaf(v[i][e], lo, __builtin_fmaf(v[i][e], hi, -t)) * w[e] : 0.f;
+            y32[e] = __builtin_fmaf(t, w[e], rest);
+            v[i][e] = to_odd(y32[e], __builtin_fmaf(t, w[e], -y32[e]) + rest);
         }
+        if (sizeof(E) == 4 && p.Y != nullptr && at + i * TPR * 8 < p.K)  // (fp32's own rounding)
+            store8(static_cast<E *>(p.Y) + row * p.ldy + at + i * TPR * 8, y32);
+        if constexpr (TPR == 1024) asm volatile("" ::: "memory");  // one piece of gamma at a time: 128 registers are all there are
+#pragma unroll
+        for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(v[i][e]));  // (here, or its parts stay in registers until the codes are made)
     }
-    if (p.Y != nullptr) {
+    if (sizeof(E) != 4 && p.Y != nullptr) {
         E *y = static_cast<E *>(p.Y) + row * p.ldy;
 #pragma unroll
         for (int i = 0; i < PCS; ++i)
@@ -280,7 +308,7 @@ hipError_t launch_norm_t(const RmsNormArgs &a, hipStream_t stream, const KernelT
 // Threads per row by its length alone, so that a row's result does not depend on how many there are.  Measured in us with 64 / 256 / 512 / 1024
 // threads (bf16 with residual, sum, normed rows and 8-bit rows): 7500 rows of 512 9.7 / 17.6 / 32 / 58; 1000 of 1024 4.2 / 4.9 / 6.2 / 9.9;
 // 1 of 4096 5.1 / 2.7 / 2.6 / 3.2; 7500 of 4096 51 / 46 / 45 / 72 (6.1 TB/s); 1500 of 5120 14.2 with 256, 14.4, 16.6; 391 of 11008 in
-// fp32 17.0 with 256, 15.6, 15.1; 100 of 16384 7.6 with 256, 7.0, 6.8.
+// fp32 17.0 with 256, 15.6, 15.1; 100 of 16384 7.6 with 256, 7.0, 6.8 (all without to_odd).
 template <typename E>
 hipError_t launch_norm_e(const RmsNormArgs &a, hipStream_t stream, const KernelTimer *timer) {
     const int pieces = a.K / 8;

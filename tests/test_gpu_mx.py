@@ -173,6 +173,22 @@ def test_norm_of_a_row_does_not_depend_on_the_others():
             assert torch.equal(some.y, every.y[:rows]) and torch.equal(some.q.codes, every.q.codes[:rows]) and torch.equal(some.q.scales, every.q.scales[:rows])
 
 
+def test_norm_rounds_the_8_bit_rows_once():
+    """Ten million elements are enough for some to lie nearer to a border between two 8-bit values than half a step of fp32
+    (one in 2^21 does): they fall where the formula in 64 bits has them.  Without a residual, whose sum is fp32's."""
+    c, rt, mx = _tools()
+    torch.manual_seed(5)
+    rows, K = 2600, 4096
+    x, g = torch.randn(rows, K, device=c.device).bfloat16(), (1 + 0.3 * torch.randn(K, device=c.device)).bfloat16()
+    n = mx.rms_norm(c, x, g, 1e-5, quantize=True)
+    _, y = ref.rms_norm(_f64(x), _f64(g), 1e-5)
+    for i in range(0, rows, 200):
+        codes, scales = ref.quantize(y[i:i + 200], "e4m3")
+        assert np.array_equal(n.q.codes[i:i + 200].cpu().numpy(), codes) and np.array_equal(n.q.scales[i:i + 200].cpu().numpy(), scales)
+    mantissa, exponent = np.frexp(y)  # (a bf16 value has 8 significant bits)
+    assert np.array_equal(_f64(n.y), np.ldexp(np.rint(mantissa * 256) / 256, exponent))
+
+
 def test_norm_special_rows():
     """Rows of zeros, with and without eps; an infinity or a NaN stays in its row; values too small to square."""
     c, rt, mx = _tools()
