@@ -81,8 +81,8 @@ typedef struct lora_rms_norm_desc {
 } lora_rms_norm_desc;
 
 /* h = X + R (X alone without R), in fp32;  y = h / sqrt(mean(h^2) + eps) * gamma, the mean in 64 bits; H and Y are h and y rounded
- * once, q is what lora_mx_quantize() would make of y before any rounding.  At least one of H, Y and q; outputs may not overlap each other, gamma, or -- but
- * for the two cases above -- the inputs.  Rows are independent, and a row's result does not depend on the others.
+ * once, q is what lora_mx_quantize() would make of y before any rounding.  At least one of H, Y and q; outputs may not
+ * overlap each other, gamma, or -- but for the two cases above -- the inputs.  Rows are independent, and a row's result does not depend on the others.
  * Asynchronous on `stream`; no-op for 0 rows.  Errors: INVALID_ARG, SHAPE, ALIGNMENT; HIP if the launch fails. */
 int lora_rms_norm(lora_ctx *ctx, const lora_rms_norm_desc *desc, lora_stream_t stream);
 
@@ -114,14 +114,15 @@ size_t lora_mx_linear_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r
 /* The layer.  Products of the held values are exact and summed in fp32; the adapter term's intermediate is rounded as
  * lora_linear() says; Y is rounded once.  (Activations in bf16 of more than 128 rows are taken apart into two parts of 8 bits:
  * exactly down to 2^-14 of the largest value of their block of 32, off by at most 2^-22 of it below.)  An infinity or a NaN among a
- * row's activations makes that row of Y infinite or NaN, one in a block of W its column.  Returns after enqueueing launches only (it may be captured into a graph as
- * lora_linear() may).  Bitwise reproducible run to run.  Errors, all found before the first launch: INVALID_ARG, PLAN,
+ * row's activations makes that row of Y infinite or NaN, one in a block of W its column.  Returns after enqueueing launches
+ * only (it may be captured into a graph as lora_linear() may).  Bitwise reproducible run to run.  Errors, all found before the first launch: INVALID_ARG, PLAN,
  * SHAPE, ALIGNMENT, WORKSPACE_TOO_SMALL; HIP if a launch fails. */
 int lora_mx_linear(lora_ctx *ctx, const lora_plan_t *plan, const lora_mx_linear_desc *desc, lora_stream_t stream);
 
 /* Several projections of the same activations in one call (1 <= n <= LORA_MAX_MULTI): descs share X, ldx, Xq and K; each has
  * its own W, N, Y, table and workspace.  Computes what n calls of lora_mx_linear() compute.  Errors as there; INVALID_ARG also
- * for n out of range, descs that differ in the activations or K, or two with overlapping Y or the same workspace. */
+ * for n out of range, descs that differ in the activations or K, or two of which one's Y or workspace overlaps the other's Y,
+ * workspace or W. */
 int lora_mx_linear_multi(lora_ctx *ctx, const lora_plan_t *plan, const lora_mx_linear_desc *const *descs, int32_t n,
                          lora_stream_t stream);
 

@@ -147,6 +147,9 @@ def test_multi_refusals():
     for kw in (dict(X=AT[0] + 16), dict(ldx=72), dict(Xq=_rows(AT[1] + 16, 64, AT[2], 4)), dict(Xq=NOQ), dict(Y=AT[5]), dict(ws=AT[6] + 256),
                dict(Y=AT[5] + 16, ldy=40)):
         assert call(_linear(), _linear(**{**other, **kw})) == B.LORA_ERR_INVALID_ARG
+    # one projection's output or workspace over another's weights
+    for w in (_rows(AT[5], 32, AT[4], 4, mx.LORA_MX_E2M1), _rows(AT[3], 32, AT[5] + 64, 4, mx.LORA_MX_E2M1), _rows(AT[6], 32, AT[4], 4, mx.LORA_MX_E2M1)):
+        assert call(_linear(), _linear(**{**other, "W": w})) == call(_linear(**{**other, "W": w}), _linear()) == B.LORA_ERR_INVALID_ARG
 
 
 def test_workspace_bytes():
