@@ -307,8 +307,9 @@ hipError_t launch_norm_t(const RmsNormArgs &a, hipStream_t stream, const KernelT
 
 // Threads per row by its length alone, so that a row's result does not depend on how many there are.  Measured in us with 64 / 256 / 512 / 1024
 // threads (bf16 with residual, sum, normed rows and 8-bit rows): 7500 rows of 512 9.7 / 17.6 / 32 / 58; 1000 of 1024 4.2 / 4.9 / 6.2 / 9.9;
-// 1 of 4096 5.1 / 2.7 / 2.6 / 3.2; 7500 of 4096 51 / 46 / 45 / 72 (one set of outputs, which the cache holds in part; 56 with three, 5.0 TB/s); 1500 of 5120 14.2 with 256, 14.4, 16.6; 391 of 11008 in
-// fp32 17.0 with 256, 15.6, 15.1; 100 of 16384 7.6 with 256, 7.0, 6.8 (all without to_odd).
+// 1 of 4096 5.1 / 2.7 / 2.6 / 3.2; 7500 of 4096 51 / 46 / 45 / 72 (one set of outputs, which the cache holds in part; 56 with three,
+// 5.0 TB/s); 1500 of 5120 14.2 with 256, 14.4, 16.6; 391 of 11008 in fp32 17.0 with 256, 15.6, 15.1; 100 of 16384 7.6 with 256, 7.0,
+// 6.8 (all without to_odd).
 template <typename E>
 hipError_t launch_norm_e(const RmsNormArgs &a, hipStream_t stream, const KernelTimer *timer) {
     const int pieces = a.K / 8;
