@@ -548,3 +548,50 @@ def test_replayed_graph_equals_eager_calls(T, x8):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, Ys)), k
         assert pl.status(c)[0] == 0
+
+
+@pytest.mark.parametrize("x8", [False, True])
+def test_two_graphs_on_one_workspace(x8):
+    """Both replayed in turn, with a bigger eager call on the same workspace in between; the outputs are the exact ones every time."""
+    c, rt, mx = _tools()
+    layers = [Layer(70, 1056, [100], (8, 16), x8, whole=True), Layer(300, 544, [333], (16,), x8, whole=True, seed=1),
+              Layer(600, 1056, [264], (24,), x8, whole=True, seed=2)]
+    want = [_bf16(a.ref[0][0])[1] for a in layers]
+    size = max(mx.lora_mx_linear_workspace_bytes(a.T, a.X.shape[1], want[i].shape[1], 32, int(x8)) for i, a in enumerate(layers))
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=c.device)
+    Ys = [torch.zeros(w.shape[0], (w.shape[1] + 7) // 8 * 8, dtype=torch.bfloat16, device=c.device)[:, :w.shape[1]] for w in want]
+    descs = [mx.linear_desc(a.plan, a.Xt, a.proj[0][0], Y, a.proj[0][1], ws, a.Xq) for a, Y in zip(layers, Ys)]
+    run = lambda i: mx.lora_mx_linear(c.handle, layers[i].plan.struct, descs[i], rt._stream())  # noqa: E731
+    side, graphs = torch.cuda.Stream(), []
+    for i in (0, 1):
+        run(i)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            run(i)
+    for k in range(3):
+        for Y in Ys:
+            Y.zero_()
+        graphs[k % 2].replay()
+        run(2)
+        graphs[1 - k % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(Y.cpu(), w) for Y, w in zip(Ys, want)), k
+
+
+@pytest.mark.parametrize("x8", [False, True])
+def test_calls_on_two_streams_at_once(x8):
+    """One context, two streams, a workspace each."""
+    c, rt, mx = _tools()
+    layers = [Layer(90, 1056, [264], (8, 16), x8, whole=True), Layer(700, 1056, [264], (16, 8), x8, whole=True, seed=1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(8):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] += layers[i].run()
+    torch.cuda.synchronize()
+    for layer, ys in zip(layers, got):
+        want = _bf16(layer.ref[0][0])[1]
+        assert all(torch.equal(Y.cpu(), want) for Y in ys)
