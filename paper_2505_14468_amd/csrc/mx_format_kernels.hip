@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_dequantize_kernel(MxConvertA
 // Roundings: squares are exact in 64 bits and summed there, and the scale of a row is kept as two fp32 numbers, so that fp32's y is off by
 // little more than its last product's half a step.  The narrower outputs are rounded from more bits than that (to_odd): from fp32's y one
 // element in 2^21 would fall to the wrong side of a border between two 8-bit values.  The 64-bit sums hide
-// behind the loads; rounding once costs 46.4 -> 47.1 us at 7500 rows of 4096, 14.9 -> 16.5 at 1500 of 5120.
+// behind the loads; rounding once costs 46.4 -> 47.1 us at 7500 rows of 4096, 14.9 -> 16.2 at 1500 of 5120.
 
 // `y` with what is missing from it folded into its last bit ("round to odd"): a later rounding to at most 22 bits then gives what rounding
 // y + rest once would give, because a border between such values has an even last bit, which only an exact y keeps.
@@ -232,9 +232,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
                     for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(v[j + i][e])::"memory");
         }
     }
+    // (whether any of the wave's lanes has a piece i; 1500 rows of 5120, where six of eight waves have no second one, 17.3 -> 16.2 us)
+    const int first = (RPW > 1 ? wave % WPR : wave) * 512;
+    auto any = [&](int i) { return i == 0 || first + i * TPR * 8 < p.K; };
     double ss = 0.0;
 #pragma unroll
     for (int i = 0; i < PCS; ++i) {
+        if (!any(i)) continue;
         double s[2] = {0.0, 0.0};
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e & 1] = __builtin_fma((double)v[i][e], (double)v[i][e], s[e & 1]);
@@ -261,6 +265,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
     }
 #pragma unroll
     for (int i = 0; i < PCS; ++i) {
+        if (!any(i)) continue;
         float w[8];
         load8(g + min(at + i * TPR * 8, p.K - 8), w);
         float y32[8];
@@ -288,6 +293,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
         unsigned char *codes = p.codes + row * p.ldc, *scales = p.scales + row * p.ldsc;
 #pragma unroll
         for (int i = 0; i < PCS; ++i) {
+            if (!any(i)) continue;
             const int k = at + i * TPR * 8;
             const int s = scale_code<kMxE4M3>(quad_max(v[i]));
             const uint2 c = codes_e4m3(v[i], inverse_scale(s));
