@@ -9,6 +9,9 @@
  * that of lora_linear(): from X in bf16, on the same plan and the same adapter tables.  Contexts, streams, plans,
  * status codes and the ownership of memory are those of lora_mi355x.h.
  *
+ * Operands overlap where they have a byte of their rows in common: rows of one stride may lie side by side in a buffer (packed
+ * projections, H and Y as halves, codes with their scales behind them).  Of different strides the extents, first byte to last, decide.
+ *
  * Formats (the layout of the OCP microscaling formats): every 32 consecutive values of a row are a block with one scale.
  *     value = element * 2^(scale - 127)          scale: one byte; 255 makes the whole block NaN
  *     LORA_MX_E2M1   elements of 4 bits, two a byte, the even one in the low half: 0 0.5 1 1.5 2 3 4 6 and their negatives

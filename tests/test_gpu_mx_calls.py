@@ -1,0 +1,53 @@
+"""Calls of the operators on block-scaled formats as programs lay out their buffers: outputs side by side, codes and scales in one buffer."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from oracle import mx_reference as ref  # noqa: E402
+from test_gpu_mx import Layer, _bf16, _check_norm, _f64, _tools  # noqa: E402
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T", [1, 73, 300])
+def test_packed_projections(T, x8):
+    """q, k and v into the columns of one buffer, which also holds 16 columns of something else: the exact results, and the rest as it was."""
+    c, rt, mx = _tools()
+    Ns = (96, 40, 200)
+    layer = Layer(T, 1056, Ns, (8, 16), x8, whole=True)
+    packed = torch.full((T, sum(Ns) + 16), 3.0, dtype=torch.bfloat16, device=c.device)
+    at = np.concatenate([[8], 8 + np.cumsum(Ns)])
+    Ys = [packed[:, i:i + n] for i, n in zip(at, Ns)]
+    ws = [mx.workspace(T, 1056, n, 16, c.device, x8) for n in Ns]
+    descs = [mx.linear_desc(layer.plan, layer.Xt, W, Y, t, w, layer.Xq) for (W, t), Y, w in zip(layer.proj, Ys, ws)]
+    mx.lora_mx_linear_multi(c.handle, layer.plan.struct, descs, rt._stream())
+    for Y, (want, _, _) in zip(Ys, layer.ref):
+        assert torch.equal(Y.cpu(), _bf16(want)[1])
+    assert (packed[:, :8] == 3).all() and (packed[:, at[-1]:] == 3).all()
+
+
+def test_norm_outputs_and_held_rows_side_by_side():
+    """H and Y as halves of one buffer; the 8-bit rows and their scales as rows of another."""
+    c, rt, mx = _tools()
+    for rows, K in ((1, 4096), (37, 1024), (300, 96)):
+        x, r, g = (torch.randn(s, device=c.device).bfloat16() for s in ((rows, K), (rows, K), (K,)))
+        both = torch.full((rows, 2 * K + 16), 3.0, dtype=torch.bfloat16, device=c.device)
+        h, y = both[:, :K], both[:, K:2 * K]
+        held = torch.full((rows, K + K // 32 // 16 * 16 + 32), 77, dtype=torch.uint8, device=c.device)
+        q = mx.MxTensor(held[:, :K], held[:, K:K + K // 32], "e4m3")
+        assert q.codes.data_ptr() == held.data_ptr() and q.scales.data_ptr() == held.data_ptr() + K
+        mx.lora_rms_norm(c.handle, mx.norm_desc(x, g, 1e-5, residual=r, h=h, y=y, q=q), rt._stream())
+        apart = mx.rms_norm(c, x, g, 1e-5, r, quantize=True)
+        assert torch.equal(h, apart.h) and torch.equal(y, apart.y) and torch.equal(q.codes, apart.q.codes) and torch.equal(q.scales, apart.q.scales)
+        assert (both[:, 2 * K:] == 3).all() and (held[:, K + K // 32:] == 77).all()
+        _check_norm(h, y, _f64(x), _f64(r), _f64(g), 1e-5, "bf16")
+        for fmt, width in (("e4m3", K), ("e2m1", K // 2)):
+            held.fill_(77)
+            q = mx.MxTensor(held[:, :width], held[:, width:width + K // 32], fmt)
+            mx.quantize(c, x, fmt, out=q)
+            codes, scales = ref.quantize(_f64(x), fmt)
+            assert np.array_equal(q.codes.cpu().numpy(), codes) and np.array_equal(q.scales.cpu().numpy(), scales)
+            assert (held[:, width + K // 32:] == 77).all()
+            assert np.array_equal(_f64(mx.dequantize(c, q)), ref.dequantize(codes, scales, fmt))
