@@ -51,3 +51,17 @@ def test_norm_outputs_and_held_rows_side_by_side():
             assert np.array_equal(q.codes.cpu().numpy(), codes) and np.array_equal(q.scales.cpu().numpy(), scales)
             assert (held[:, width + K // 32:] == 77).all()
             assert np.array_equal(_f64(mx.dequantize(c, q)), ref.dequantize(codes, scales, fmt))
+
+
+def test_no_rows():
+    c, rt, mx = _tools()
+    x, g = torch.empty(0, 64, dtype=torch.bfloat16, device=c.device), torch.ones(64, dtype=torch.bfloat16, device=c.device)
+    pl = rt.plan(c, np.zeros(1, np.int32), np.zeros(1, np.int32), np.array([8], np.int32))
+    W = mx.quantize(c, torch.randn(40, 64, device=c.device), "e2m1")
+    for q8 in (False, True):
+        n = mx.rms_norm(c, x, g, 1e-5, x, quantize=q8)
+        assert n.y.shape == n.h.shape == (0, 64) and (n.q is None) == (not q8)
+        assert mx.rms_norm(c, x, g, 1e-5, quantize=True, normed=False).q.shape == (0, 64)
+        h, outs = mx.norm_linear_multi(c, pl, x, x, g, 1e-5, [(W, None), (W, None)], x8=q8)
+        assert h.shape == (0, 64) and all(Y.shape == (0, 40) for Y in outs)
+    assert mx.dequantize(c, mx.quantize(c, x, "e2m1")).shape == (0, 64)
