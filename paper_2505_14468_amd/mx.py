@@ -158,7 +158,7 @@ _NONE = lora_mx_rows_t(None, 0, None, 0, LORA_MX_E4M3, 0)
 
 def _ld(t: torch.Tensor) -> int:
     assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "rows are contiguous"
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (t.shape[1] + 7) // 8 * 8)
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8  # (the stride of a single row says nothing)
 
 
 def quantize_desc(X: torch.Tensor, q: MxTensor) -> lora_mx_convert_desc:
