@@ -102,7 +102,8 @@ __global__ __launch_bounds__(kMxWaves * 64) void mx_quantize_kernel(MxConvertArg
 // A bf16 row as the sum of two e4m3 rows: the first is the row's quantization, the second that of what it leaves, with a scale
 // 2^-4 of the first's (a remainder is at most half a step of the first, 2^-4 of 256 .. 448 there).  bf16 has 8 significant bits and each
 // part holds 4, so the sum is the value itself where the second part's smallest step, 2^-13 of the first scale, is not above the
-// value's own -- down to 2^-14 of its block's largest -- and off by at most 2^-22 of that largest value below.
+// value's own -- down to 2^-6 of that scale -- and off by at most half of that step, 2^-14 of the scale, below.  The block's largest
+// value is above 224 scales: exact down to 2^-13 of it, off by less than 2^-21 of it below (2^-13.8 and 2^-21.8 where it is just above).
 __global__ __launch_bounds__(kMxWaves * 64) void mx_split_kernel(MxSplitArgs p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned unit = workgroup() * kMxWaves + wave, urow = unit / (unsigned)p.strips;
