@@ -117,7 +117,8 @@ size_t lora_mx_linear_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r
 /* The layer.  Products of the held values are exact and summed in fp32; the adapter term's intermediate is rounded as
  * lora_linear() says; Y is rounded once.  (Activations in bf16 of more than 128 rows are taken apart into two parts of 8 bits:
  * exactly down to 2^-13 of the largest value of their block of 32, off by at most 2^-21 of it below.)  An infinity or a NaN among a
- * row's activations makes that row of Y infinite or NaN, one in a block of W its column.  Returns after enqueueing launches
+ * row's activations makes that row of Y infinite or NaN, one in a block of W its column, one in an adapter the rows that use it; above 128 rows
+ * one in B_a may reach the rows that share a block of 16 with those in the plan's order, and no others.  Returns after enqueueing launches
  * only (it may be captured into a graph as lora_linear() may).  Bitwise reproducible run to run.  Errors, all found before the first launch: INVALID_ARG, PLAN,
  * SHAPE, ALIGNMENT, WORKSPACE_TOO_SMALL; HIP if a launch fails. */
 int lora_mx_linear(lora_ctx *ctx, const lora_plan_t *plan, const lora_mx_linear_desc *desc, lora_stream_t stream);
