@@ -201,6 +201,13 @@ __device__ __forceinline__ float to_odd(float y, float rest) {
     return __builtin_amdgcn_classf(rest, 0x108) ? __int_as_float((bits + back) | 1) : y;
 }
 
+// What all lanes of the wave hold, in scalar registers.
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+__device__ __forceinline__ double uniform(double v) {
+    const long long b = __double_as_longlong(v);
+    return __hiloint2double(__builtin_amdgcn_readfirstlane((int)(b >> 32)), __builtin_amdgcn_readfirstlane((int)b));
+}
+
 template <typename E, int TPR, int PCS>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNormArgs p) {
     constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR, WPR = TPR / 64;
@@ -255,8 +262,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
         for (int w = 0; w < WPR; ++w) ss += part[(RPW > 1 ? wave / WPR * WPR : 0) + w];
     }
     if (!mine) return;
-    const double scale = 1.0 / __builtin_sqrt(ss / (double)p.K + (double)p.eps);
-    const float hi = (float)scale, lo = __builtin_isfinite(hi) ? (float)(scale - (double)hi) : 0.f;
+    double scale = uniform(1.0 / __builtin_sqrt(ss / (double)p.K + (double)p.eps));  // (the row's, so the wave's: scalar registers)
     // (whatever is stored is stored behind the row's last load: H and Y may be X or R)
     if (p.H != nullptr) {
         E *h = static_cast<E *>(p.H) + row * p.ldh;
@@ -264,6 +270,17 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(RmsNorm
         for (int i = 0; i < PCS; ++i)
             if (at + i * TPR * 8 < p.K) store8(h + at + i * TPR * 8, v[i]);
     }
+    // (rows below 2^-120 or above 2^100, whose scale or the second part of it is no normal number of fp32: a power of two goes from the scale
+    // into the values, exactly where y is above 2^-100)
+    if (scale > 0x1p120 || scale < 0x1p-100) {
+        const float shift = scale > 1.0 ? 0x1p64f : 0x1p-32f;
+        scale *= scale > 1.0 ? 0x1p-64 : 0x1p32;
+#pragma unroll
+        for (int i = 0; i < PCS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] *= shift;
+    }
+    const float hi = uniform((float)scale), lo = uniform(__builtin_isfinite(hi) ? (float)(scale - (double)hi) : 0.f);
 #pragma unroll
     for (int i = 0; i < PCS; ++i) {
         if (!any(i)) continue;
