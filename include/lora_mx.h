@@ -108,10 +108,12 @@ typedef struct lora_mx_linear_desc {
     size_t workspace_bytes;
 } lora_mx_linear_desc;
 
-/* Device bytes lora_mx_linear() needs in desc->workspace (with_xq: whether Xq is given): lora_linear()'s preferred size; above 128
- * rows also the activations in two parts of 8 bits (bf16 ones: 2 T bytes for every K, rounded up to whole 512, and 1/32 of that), and
- * partial sums in fp32 where the tiles alone would leave much of the chip idle.  One workspace may serve calls of different shapes
- * as long as it is big enough for each and they do not overlap in time.  0 for invalid arguments. */
+/* A size of desc->workspace in device bytes that serves every lora_mx_linear() of this K and N on up to T rows and ranks up to r_max (with_xq: whether
+ * Xq is given; the size without it serves calls with it too).  It holds what lora_linear()'s does (V, the decode path's partial sums of up
+ * to 128 rows, the adapter term in fp32); above 128 rows also the activations in two parts of 8 bits (bf16 ones: 2 T bytes for every K, rounded
+ * up to whole 512, and 1/32 of that), and partial sums in fp32 where the tiles of T rows alone would leave much of the chip idle.  (A
+ * batch that would want more room for those than is left is cut into fewer stretches of K, or none.)  One workspace may serve calls of
+ * different shapes as long as it is big enough for each and they do not overlap in time.  0 for invalid arguments. */
 size_t lora_mx_linear_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r_max, int32_t with_xq);
 
 /* The layer.  Products of the held values are exact and summed in fp32; the adapter term's intermediate is rounded as

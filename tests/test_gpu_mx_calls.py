@@ -65,3 +65,41 @@ def test_no_rows():
         h, outs = mx.norm_linear_multi(c, pl, x, x, g, 1e-5, [(W, None), (W, None)], x8=q8)
         assert h.shape == (0, 64) and all(Y.shape == (0, 40) for Y in outs)
     assert mx.dequantize(c, mx.quantize(c, x, "e2m1")).shape == (0, 64)
+
+
+@pytest.mark.parametrize("x8", [False, True])
+def test_one_workspace_for_every_batch(x8):
+    """Sized once for the largest batch, as a serving loop does; what lies behind it stays as it was."""
+    c, rt, mx = _tools()
+    K, N, most = 2080, 264, 1500
+    n = mx.lora_mx_linear_workspace_bytes(most, K, N, 24, int(x8))
+    room = torch.full((n + 4096,), 255, dtype=torch.uint8, device=c.device)
+    for T in (most, 700, 391, 300, 129, 128, 100, 17, 1):
+        layer = Layer(T, K, [N], (8, 24), x8, whole=True)
+        for expand in (-1, 0, 1):
+            c.set_option("expand_split", expand)
+            try:
+                Y = mx.linear(c, layer.plan, layer.Xt, *layer.proj[0], Xq=layer.Xq, ws=room[:n])
+            finally:
+                c.set_option("expand_split", -1)
+            assert torch.equal(Y.cpu(), _bf16(layer.ref[0][0])[1]), T
+        assert (room[n:] == 255).all()
+
+
+def test_smallest_workspace():
+    """The smallest workspace that is taken, found by its refusals: K in one stretch, the exact result, nothing behind it touched."""
+    c, rt, mx = _tools()
+    for T, K, N in ((391, 4128, 264), (160, 2080, 40), (100, 1056, 40)):
+        for x8 in (False, True):
+            layer = Layer(T, K, [N], (8, 24), x8, whole=True)
+            W, table = layer.proj[0]
+            hi = mx.lora_mx_linear_workspace_bytes(T, K, N, 24, int(x8))
+            room = torch.full((hi + 4096,), 255, dtype=torch.uint8, device=c.device)
+            Y = torch.zeros(T, N, dtype=torch.bfloat16, device=c.device)
+            status = lambda n: mx.lora_mx_linear(None, layer.plan.struct, mx.linear_desc(layer.plan, layer.Xt, W, Y, table, room[:n], layer.Xq), 0, raw=True)  # noqa: E731
+            lo = 0  # (no context: nothing is launched)
+            while lo < hi:
+                mid = (lo + hi) // 2
+                lo, hi = (mid + 1, hi) if status(mid) == rt.B.LORA_ERR_WORKSPACE_TOO_SMALL else (lo, mid)
+            mx.linear(c, layer.plan, layer.Xt, W, table, Xq=layer.Xq, Y=Y, ws=room[:lo])
+            assert torch.equal(Y.cpu(), _bf16(layer.ref[0][0])[1]) and (room[lo:] == 255).all()
