@@ -103,3 +103,23 @@ def test_smallest_workspace():
                 lo, hi = (mid + 1, hi) if status(mid) == rt.B.LORA_ERR_WORKSPACE_TOO_SMALL else (lo, mid)
             mx.linear(c, layer.plan, layer.Xt, W, table, Xq=layer.Xq, Y=Y, ws=room[:lo])
             assert torch.equal(Y.cpu(), _bf16(layer.ref[0][0])[1]) and (room[lo:] == 255).all()
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T", [1, 31, 128, 150, 420])
+def test_projections_with_and_without_adapters(T, x8):
+    """Some of the projections have a table and some have none, the first one either way; the term in the tiles and from memory."""
+    c, rt, mx = _tools()
+    layer = Layer(T, 1056, (64, 200, 33, 40), (8, 16, 512), x8, whole=True)
+    for have in ((0, 2), (1,), (1, 3), (0, 1, 2, 3), ()):
+        for expand in (-1, 0, 1):
+            c.set_option("expand_split", expand)
+            try:
+                outs = mx.linear_multi(c, layer.plan, layer.Xt, [(W, t if i in have else None) for i, (W, t) in enumerate(layer.proj)], Xq=layer.Xq)
+            finally:
+                c.set_option("expand_split", -1)
+            for i, (Y, (W, _), (want, S, _)) in enumerate(zip(outs, layer.proj, layer.ref)):
+                assert S.max() < 2 ** 24
+                if i not in have:
+                    want = layer.Xb @ ref.dequantize(W.codes.cpu().numpy(), W.scales.cpu().numpy(), "e2m1").T
+                assert torch.equal(Y.cpu(), _bf16(want)[1]), (have, expand, i)
