@@ -499,8 +499,9 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs &p, int m0, int pn
                 }
             }
         } else {
-            // The term is read AHEAD row blocks before the stores that it is added into, and only where a block holds such a row (1216
-            // rows of which 192 take it, 4096 -> 11008: 60 us with one block ahead and every block read).
+            // The term is read AHEAD row blocks before the stores that it is added into, and only where a block holds such a row: 8 MB instead of
+            // 53 at 1216 rows of which 186 take it, 4096 -> 11008.  The time there is the same, 64.9 us and 64.3 with one block ahead and every
+            // block read: it is the chain of reads at the tile's end, 8.5 us over a table that no row uses (56), that costs.
             constexpr int AHEAD = NBT > 4 ? 3 : 2;
             chunk_t term[AHEAD + 1][2 * NP];
             auto fetch = [&](int tb, chunk_t(&d)[2 * NP]) __attribute__((always_inline)) {

@@ -111,8 +111,9 @@ def lora_mx_linear_multi(ctx, plan, descs, stream: int, *, raw: bool = False):
 
 class MxTensor:
     """``rows`` x ``K`` values in a block-scaled format: ``codes`` (uint8, [rows, K] of e4m3 or [rows, K / 2] of e2m1, the even value
-    in the low half) and ``scales`` (uint8, [rows, K / 32], 127 = 1).  Tensors are taken as they are, rows of any stride; scales
-    whose rows are not a multiple of 4 bytes apart are copied into rows that are."""
+    in the low half) and ``scales`` (uint8, [rows, K / 32], 127 = 1).  Tensors are taken as they are where the kernels can read them: rows
+    of codes at multiples of 16 bytes, rows of scales at multiples of 4.  Others are copied into such rows, which ``self.codes`` and
+    ``self.scales`` then are, also for what an operator writes."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, fmt: str):
         self.format = fmt
