@@ -123,3 +123,26 @@ def test_projections_with_and_without_adapters(T, x8):
                 if i not in have:
                     want = layer.Xb @ ref.dequantize(W.codes.cpu().numpy(), W.scales.cpu().numpy(), "e2m1").T
                 assert torch.equal(Y.cpu(), _bf16(want)[1]), (have, expand, i)
+
+
+@pytest.mark.parametrize("T", [1, 90, 300])
+def test_inputs_beside_the_output(T):
+    """A buffer whose rows hold the 8-bit codes, their scales, the bf16 activations and the output, one behind the other: what is read past
+    the end of a row's codes is the output that is being written."""
+    c, rt, mx = _tools()
+    K, N = 544, 72
+    layer = Layer(T, K, [N], (8, 16), True, whole=True)
+    at = {"Y": K, "scales": K + 2 * N, "X": K + 2 * N + 32}
+    width = at["X"] + 2 * K + 32
+    buf = torch.full((T, width), 255, dtype=torch.uint8, device=c.device)
+    wide = buf.view(torch.bfloat16)
+    Y, X = wide[:, at["Y"] // 2:at["Y"] // 2 + N], wide[:, at["X"] // 2:at["X"] // 2 + K]
+    X.copy_(layer.Xt)
+    buf[:, :K], buf[:, at["scales"]:at["scales"] + K // 32] = layer.Xq.codes, layer.Xq.scales
+    Xq = mx.MxTensor(buf[:, :K], buf[:, at["scales"]:at["scales"] + K // 32], "e4m3")
+    assert Xq.codes.data_ptr() == buf.data_ptr() and Xq.scales.data_ptr() == buf.data_ptr() + at["scales"]
+    before = buf.clone()
+    mx.linear(c, layer.plan, X, *layer.proj[0], Xq=Xq, Y=Y)
+    assert torch.equal(Y.cpu(), _bf16(layer.ref[0][0])[1])
+    buf[:, at["Y"]:at["Y"] + 2 * N] = before[:, at["Y"]:at["Y"] + 2 * N]
+    assert torch.equal(buf, before)
