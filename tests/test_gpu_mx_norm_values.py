@@ -46,8 +46,8 @@ def test_every_output_is_rounded_once(K, dtype):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("K", LENGTHS)
 def test_rows_of_any_size(K, dtype):
-    """A row's scale may lie outside of fp32's normal numbers, or of fp32 altogether: with eps 0, rows of 2^-140 (multiples of 2^-149 in fp32,
-    of 2^-133 in bf16) to 2^126, and one with a single smallest value among zeros."""
+    """A row's scale may lie outside of fp32's normal numbers, or of fp32 altogether: with eps 0, rows of 2^-130 (multiples of 2^-149 in fp32,
+    of 2^-133 in bf16) to 2^125, and one with a single smallest value among zeros."""
     c, rt, mx = _tools()
     torch.manual_seed(K)
     sizes = torch.tensor([2.0 ** e for e in (-130, -128, -125, -121, -119, -100, 0, 90, 99, 101, 119, 121, 125)], dtype=torch.float64)
